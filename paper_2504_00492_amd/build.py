@@ -1,4 +1,4 @@
-"""Builds the gfx950 shared library (libpf.so) in-tree with hipcc.
+"""Builds the gfx950 shared libraries (libpf.so, libpf_layer.so) in-tree with hipcc.
 
 `python -m paper_2504_00492_amd.build` or `build_library()`.  Cross-compiles without a GPU.
 """
@@ -12,6 +12,9 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpf.so")
+# the operators around the delta rule, a library of their own: who runs the recurrence alone does not load them
+LAYER_LIB = os.path.join(HERE, "libpf_layer.so")
+LAYER_SOURCES = ["pf_layer_api.hip", "pf_norm.hip", "pf_quant.hip", "pf_matmul.hip", "pf_gated.hip"]
 SOURCES = ["pf_api.hip", "pf_generic.hip", "pf_flow.hip", "pf_scan.hip", "pf_fused.hip", "pf_segments.hip", "pf_sigdelta.hip", "pf_rescale.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Packed-fp32 VALU forms are switched off for every kernel of this library.  The feature flag
@@ -36,12 +39,14 @@ def _compile(src: str) -> str:
 
 
 def build_library(verbose: bool = False) -> str:
-    """Compile every source and link libpf.so.  Always recompiles."""
-    with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
-        objs = list(ex.map(_compile, SOURCES))
-    subprocess.run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs], check=True)
+    """Compile every source and link libpf.so and libpf_layer.so.  Always recompiles."""
+    with ThreadPoolExecutor(max_workers=8) as ex:
+        objs = list(ex.map(_compile, SOURCES + LAYER_SOURCES))
+    link = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC"]
+    subprocess.run([*link, "-o", LIB, *objs[:len(SOURCES)]], check=True)
+    subprocess.run([*link, "-o", LAYER_LIB, *objs[len(SOURCES):], "-L" + HERE, "-lpf", "-Wl,-rpath,$ORIGIN"], check=True)
     if verbose:
-        print("built", LIB, file=sys.stderr)
+        print("built", LIB, "and", LAYER_LIB, file=sys.stderr)
     return LIB
 
 
