@@ -1,4 +1,19 @@
-// Gated linear recurrence h_t = a_t h_{t-1} + b_t for every sequence and channel, and its backward.
+// Gated linear recurrence h_t = a_t h_{t-1} + b_t for every sequence and channel, and its backward, whose recurrence runs
+// the other way: with m = a_{t+1} l_{t+1} coming in, l_t = dy_t + m and a_t l_t goes out.
+//
+// A span of steps takes what comes in, v, to A v + H: A the product of its gates, H what it makes of zero.  Spans join as
+// (A, H) then (A', H') = (A' A, A' H + H'), so they can be read side by side.  A wavefront holds 64 V channels of kSteps
+// consecutive steps in registers, a workgroup kWaves such spans, one behind the other: a tile.  Each span's (A, H) is formed first, the
+// spans in front are put through it, and the steps run once more from what really comes in.  Memory sees every array once.
+//
+// Many sequences and channels: a workgroup walks along a chain (64 V channels of one sequence) from tile to tile, the
+// next one's values on their way.  Few: every tile has a workgroup.  A tile tells the (A, H) of its channels as soon as
+// it has read them, looks back for the nearest tile in front whose outgoing values are told, runs these through the (A, H) of
+// the tiles between, and tells its own outgoing values.  A word that is told stands for itself (clear is a pattern that no
+// value has), 8 bytes in one store, so no fence orders anything.  Tiles are handed out by a counter, all chains' first tiles first: a
+// workgroup waits only for tiles handed out before its own, whose workgroups are on the chip already and wait for nothing later, so
+// every wait ends.  What a tile makes of the values that come in depends on the tiles between them in order, whichever were told, so the bits
+// do not depend on timing.
 #include "pf_layer_common.h"
 #include "pf_layer_internal.h"
 
@@ -8,81 +23,453 @@ namespace pf {
 
 namespace {
 
+constexpr int kWaves = 8, kSteps = 16, kTile = kWaves * kSteps;
+constexpr int kBehind = 8;      // tiles in front that are looked at together
+
 // the decay a, 1 - a, and d a / d g of a gate's value
 struct Gate { float a, rest, slope; };
-__device__ __forceinline__ Gate gate_of(float g, int form)
+__device__ __forceinline__ float exponential(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+// form and mix are the same for a whole launch; what is not used of the result is not computed
+__device__ __forceinline__ Gate gate_of(float g, int form, bool mix)
 {
     if (form == 0) return {g, 1.f - g, 1.f};
     if (form == 1) {
-        const float a = expf(g);
-        return {a, -expm1f(g), a};
+        const float a = exponential(g);
+        float rest = 0.f;
+        if (mix) {      // 1 - e^g: near zero the series, whose first term left out is 2e-8 of it
+            float p = 1.f / 5040;
+            p = fmaf(p, g, 1.f / 720);
+            p = fmaf(p, g, 1.f / 120);
+            p = fmaf(p, g, 1.f / 24);
+            p = fmaf(p, g, 1.f / 6);
+            p = fmaf(p, g, 0.5f);
+            p = fmaf(p, g, 1.f);
+            rest = fabsf(g) < 0.35f ? -p * g : 1.f - a;
+        }
+        return {a, rest, a};
     }
-    const float a = 1.f / (1.f + expf(-g)), rest = 1.f / (1.f + expf(g));
-    return {a, rest, a * rest};
+    const float e = exponential(-fabsf(g)), s = __builtin_amdgcn_rcpf(1.f + e), t = e * s;
+    return {g < 0.f ? t : s, g < 0.f ? s : t, t * s};
 }
 
-template <typename T>
-__global__ __launch_bounds__(64) void gated_fwd_kernel(Gated a)
+// what a span makes of v; nothing coming in stays nothing where the product of the gates is beyond fp32
+__device__ __forceinline__ float through(float A, float H, float v) { return v == 0.f ? H : fmaf(A, v, H); }
+
+// V neighbouring channels of one token
+template <typename T, int V> struct Raw { uint32_t w[(sizeof(T) * V + 3) / 4]; };
+template <typename T, int V, bool VEC> __device__ __forceinline__ Raw<T, V> fetch(const T *p, int left)
 {
-    const int groups = (a.D + 63) / 64, b = blockIdx.x / groups, c = (blockIdx.x % groups) * 64 + threadIdx.x;
-    if (c >= a.D) return;
-    const T *X = static_cast<const T *>(a.X) + b * a.xb + c, *G = static_cast<const T *>(a.G) + b * a.gb + c;
-    T *Y = static_cast<T *>(a.Y) + (long long)b * a.L * a.D + c;
-    const long long s = (long long)b * a.D + c;
-    float h = a.h0 ? a.h0[s] : 0.f;
-#pragma unroll 8
-    for (long long t = 0; t < a.L; ++t) {
-        const Gate k = gate_of((float)G[t * a.gt], a.gate);
-        const float x = (float)X[t * a.xt];
-        h = fmaf(k.a, h, a.mix ? k.rest * x : x);
-        Y[t * a.D] = (T)h;
+    Raw<T, V> r = {};
+    if constexpr (VEC) {
+        if (left > 0) __builtin_memcpy(&r, __builtin_assume_aligned(p, sizeof(T) * V), sizeof(T) * V);
+    } else {
+        T e[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) e[v] = v < left ? p[v] : (T)0.f;
+        __builtin_memcpy(&r, e, sizeof(e));
     }
-    if (a.hL) a.hL[s] = h;
+    return r;
+}
+template <typename T, int V> __device__ __forceinline__ float value(const Raw<T, V> &r, int v)
+{
+    if constexpr (sizeof(T) == 4) return __uint_as_float(r.w[v]);
+    return __uint_as_float(v % 2 ? r.w[v / 2] & 0xffff0000u : r.w[v / 2] << 16);
+}
+template <typename T, int V, bool VEC> __device__ __forceinline__ void keep(T *p, const float (&f)[V], int left)
+{
+    T e[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) e[v] = (T)f[v];
+    if constexpr (VEC) {
+        if (left > 0) __builtin_memcpy(__builtin_assume_aligned(p, sizeof(T) * V), e, sizeof(e));
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v < left) p[v] = e[v];
+    }
 }
 
-template <typename T>
-__global__ __launch_bounds__(64) void gated_bwd_kernel(Gated a)
+// words between workgroups
+constexpr uint32_t kClear = 0xffffffffu;
+__device__ __forceinline__ uint32_t told(float f)
 {
-    const int groups = (a.D + 63) / 64, b = blockIdx.x / groups, c = (blockIdx.x % groups) * 64 + threadIdx.x;
-    if (c >= a.D) return;
-    const T *X = static_cast<const T *>(a.X) + b * a.xb + c, *G = static_cast<const T *>(a.G) + b * a.gb + c;
-    const T *dY = static_cast<const T *>(a.dY) + b * a.dyb + c;
-    const long long at = (long long)b * a.L * a.D + c, s = (long long)b * a.D + c;
-    const T *Y = static_cast<const T *>(a.Yin) + at;
-    T *dX = static_cast<T *>(a.dX) + at, *dG = static_cast<T *>(a.dG) + at;
-    const float h0 = a.h0 ? a.h0[s] : 0.f;
-    float back = a.dhL ? a.dhL[s] : 0.f;      // a_{t+1} l_{t+1}
-#pragma unroll 8
-    for (long long t = a.L - 1; t >= 0; --t) {
-        const Gate k = gate_of((float)G[t * a.gt], a.gate);
-        const float l = (float)dY[t * a.dyt] + back;
-        float h = t > 0 ? (float)Y[(t - 1) * a.D] : h0;
-        if (a.mix) h -= (float)X[t * a.xt];
-        dX[t * a.D] = (T)(a.mix ? k.rest * l : l);
-        dG[t * a.D] = (T)(l * h * k.slope);
-        back = k.a * l;
+    const uint32_t u = __float_as_uint(f);
+    return u == kClear ? 0x7fc00000u : u;      // (a NaN all the same)
+}
+template <typename W> __device__ __forceinline__ void tell(W *p, W w) { __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename W> __device__ __forceinline__ W hear(const W *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+struct Work {
+    uint32_t *next;          // the counter that hands out tiles
+    unsigned long long *span; // [tile][channel] A, H
+    uint32_t *out;           // [tile][channel] what goes out
+};
+
+// steps of a chain in the order of the recurrence: step s is token s, or of the backward token L - 1 - s
+template <typename T, int V, bool VEC, bool BACK> struct Chain {
+    const Gated &a;
+    const T *x, *g, *dy, *yin;      // (of the wavefront's first channel: the same for all lanes)
+    T *o0, *o1;
+    const float *in;
+    float *out;
+    long long state;
+    int left;           // channels from this lane's first on
+    unsigned mine;      // this lane's first
+    __device__ __forceinline__ Chain(const Gated &a_, int chain, int groups, int lane) : a(a_)
+    {
+        const long long b = chain / groups;
+        const int c = (chain % groups) * (64 * V);
+        mine = lane * V;
+        left = a.D - c - (int)mine;
+        const long long at = b * a.L * a.D + c;
+        state = b * a.D + c + mine;
+        x = static_cast<const T *>(a.X) + (a.X ? b * a.xb + c : 0);
+        g = static_cast<const T *>(a.G) + b * a.gb + c;
+        if constexpr (BACK) {
+            dy = static_cast<const T *>(a.dY) + b * a.dyb + c;
+            yin = static_cast<const T *>(a.Yin) + at;
+            o0 = static_cast<T *>(a.dX) + at;
+            o1 = static_cast<T *>(a.dG) + at;
+            in = a.dhL;
+            out = a.dh0;
+        } else {
+            o0 = static_cast<T *>(a.Y) + at;
+            in = a.h0;
+            out = a.hL;
+        }
     }
-    if (a.dh0) a.dh0[s] = back;
+    __device__ __forceinline__ void incoming(float (&v)[V]) const
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = in && i < left ? in[state + i] : 0.f;
+    }
+    __device__ __forceinline__ void outgoing(const float (&v)[V]) const
+    {
+        if (out)
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (i < left) out[state + i] = v[i];
+    }
+};
+
+template <typename T, int V, bool VEC, bool BACK, int N> struct Span;
+
+// forward: N steps in registers
+template <typename T, int V, bool VEC, int N> struct Span<T, V, VEC, false, N> {
+    using C = Chain<T, V, VEC, false>;
+    Raw<T, V> x[N], g[N];
+    float a[N][V], b[N][V];
+    __device__ __forceinline__ void read(const C &c, int s0)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const long long t = s0 + i;
+            const int left = t < c.a.L ? c.left : 0;
+            x[i] = fetch<T, V, VEC>(c.x + t * c.a.xt + c.mine, left);
+            g[i] = fetch<T, V, VEC>(c.g + t * c.a.gt + c.mine, left);
+        }
+    }
+    __device__ __forceinline__ void gates(const C &c, int s0, float (&A)[V], float (&H)[V])
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v) A[v] = 1.f, H[v] = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const Gate k = gate_of(value(g[i], v), c.a.gate, c.a.mix);
+                const float in = value(x[i], v);
+                a[i][v] = s0 + i < c.a.L ? k.a : 1.f;
+                b[i][v] = s0 + i < c.a.L ? (c.a.mix ? k.rest * in : in) : 0.f;
+                A[v] *= a[i][v];
+                H[v] = fmaf(a[i][v], H[v], b[i][v]);
+            }
+    }
+    __device__ __forceinline__ void run(const C &c, int s0, float (&v)[V])
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = fmaf(a[i][j], v[j], b[i][j]);
+            if (s0 + i < c.a.L) keep<T, V, VEC>(c.o0 + (long long)(s0 + i) * c.a.D + c.mine, v, c.left);
+        }
+    }
+};
+
+template <typename T, int V, bool VEC, int N> struct Span<T, V, VEC, true, N> {
+    using C = Chain<T, V, VEC, true>;
+    Raw<T, V> x[N], g[N], dy[N], y[N];
+    __device__ __forceinline__ void read(const C &c, int s0)
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const long long t = (long long)c.a.L - 1 - s0 - i;
+            const int left = t >= 0 ? c.left : 0;
+            g[i] = fetch<T, V, VEC>(c.g + t * c.a.gt + c.mine, left);
+            dy[i] = fetch<T, V, VEC>(c.dy + t * c.a.dyt + c.mine, left);
+            y[i] = fetch<T, V, VEC>(c.yin + (t - 1) * c.a.D + c.mine, t > 0 ? c.left : 0);
+            if (c.a.mix) x[i] = fetch<T, V, VEC>(c.x + t * c.a.xt + c.mine, left);
+        }
+    }
+    __device__ __forceinline__ void gates(const C &c, int s0, float (&A)[V], float (&H)[V])
+    {
+#pragma unroll
+        for (int v = 0; v < V; ++v) A[v] = 1.f, H[v] = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float a = s0 + i < c.a.L ? gate_of(value(g[i], v), c.a.gate, false).a : 1.f;
+                A[v] *= a;
+                H[v] = a * (value(dy[i], v) + H[v]);
+            }
+    }
+    __device__ __forceinline__ void run(const C &c, int s0, float (&v)[V])
+    {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const long long t = (long long)c.a.L - 1 - s0 - i;
+            if (t < 0) break;
+            float dx[V], dg[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const Gate k = gate_of(value(g[i], j), c.a.gate, c.a.mix);
+                const float l = value(dy[i], j) + v[j];
+                float h = t > 0 ? value(y[i], j) : c.a.h0 && j < c.left ? c.a.h0[c.state + j] : 0.f;
+                if (c.a.mix) h -= value(x[i], j);
+                dx[j] = c.a.mix ? k.rest * l : l;
+                dg[j] = l * h * k.slope;
+                v[j] = k.a * l;
+            }
+            keep<T, V, VEC>(c.o0 + t * c.a.D + c.mine, dx, c.left);
+            keep<T, V, VEC>(c.o1 + t * c.a.D + c.mine, dg, c.left);
+        }
+    }
+};
+
+struct Pair { float A, H; };
+
+// A workgroup for each chain, from tile to tile.
+template <typename T, int V, bool VEC, bool BACK>
+__global__ __launch_bounds__(64 * kWaves) void gated_walk_kernel(Gated a, int groups)
+{
+    __shared__ Pair spans[2][kWaves][V][64];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Chain<T, V, VEC, BACK> c(a, blockIdx.x, groups, lane);
+    float in[V];
+    c.incoming(in);
+    Span<T, V, VEC, BACK, kSteps> s;
+    for (int s0 = 0, turn = 0; s0 < a.L; s0 += kTile, turn ^= 1) {
+        const int mine = s0 + w * kSteps;
+        s.read(c, mine);
+        float A[V], H[V];
+        s.gates(c, mine, A, H);
+#pragma unroll
+        for (int v = 0; v < V; ++v) spans[turn][w][v][lane] = {A[v], H[v]};
+        __syncthreads();
+        float now[V];
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (i == w) now[v] = in[v];
+                const Pair p = spans[turn][i][v][lane];
+                in[v] = through(p.A, p.H, in[v]);
+            }
+        }
+        s.run(c, mine, now);
+        if (s0 + kTile >= a.L && w == kWaves - 1) c.outgoing(now);
+    }
+}
+
+// A workgroup for each tile.
+template <typename T, int V, bool VEC, bool BACK>
+__global__ __launch_bounds__(64 * kWaves) void gated_tile_kernel(Gated a, int groups, int chains, int tiles, Work work)
+{
+    __shared__ Pair spans[kWaves][V][64];
+    __shared__ float come[V][64];
+    __shared__ uint32_t ticket;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (threadIdx.x == 0) ticket = __hip_atomic_fetch_add(work.next, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u;
+    __syncthreads();
+    const uint32_t id = __builtin_amdgcn_readfirstlane(ticket);
+    const int tile = id / chains, chain = id % chains, s0 = tile * kTile, mine = s0 + w * kSteps;
+    const Chain<T, V, VEC, BACK> c(a, chain, groups, lane);
+    Span<T, V, VEC, BACK, kSteps> s;
+    s.read(c, mine);
+    float A[V], H[V];
+    s.gates(c, mine, A, H);
+#pragma unroll
+    for (int v = 0; v < V; ++v) spans[w][v][lane] = {A[v], H[v]};
+    __syncthreads();
+    if (w == 0) {
+        // words of a tile of this chain lie side by side: [tile][chain][v][lane]
+        const long long row = (long long)chains * (64 * V), at = (long long)tile * row + (long long)chain * (64 * V) + lane;
+#pragma unroll
+        for (int i = 1; i < kWaves; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const Pair p = spans[i][v][lane];
+                A[v] *= p.A;
+                H[v] = fmaf(p.A, H[v], p.H);
+            }
+        float in[V];
+        if (tile == 0) {
+            c.incoming(in);
+        } else {
+            if (tile < tiles - 1)
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    tell(work.span + at + 64 * v, (unsigned long long)told(H[v]) << 32 | told(A[v]));
+            int from;      // the nearest tile that has told for all of this wavefront's channels
+            while (true) {
+                uint32_t o[kBehind][V];
+#pragma unroll
+                for (int k = 0; k < kBehind; ++k)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) o[k][v] = hear(work.out + at + 64 * v - (long long)min(k + 1, tile) * row);
+                from = -1;
+#pragma unroll
+                for (int k = kBehind - 1; k >= 0; --k) {
+                    bool ready = k < tile;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) ready = ready && o[k][v] != kClear;
+                    if (__all(ready)) {
+                        from = k;
+#pragma unroll
+                        for (int v = 0; v < V; ++v) in[v] = __uint_as_float(o[k][v]);
+                    }
+                }
+                if (from >= 0) break;
+                __builtin_amdgcn_s_sleep(1);
+            }
+            unsigned long long p[kBehind - 1][V];
+#pragma unroll
+            for (int k = 0; k < kBehind - 1; ++k)
+                if (k < from)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) p[k][v] = hear(work.span + at + 64 * v - (k + 1) * row);
+#pragma unroll
+            for (int k = kBehind - 2; k >= 0; --k)
+                if (k < from)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        while ((uint32_t)p[k][v] == kClear) p[k][v] = hear(work.span + at + 64 * v - (k + 1) * row);
+                        in[v] = through(__uint_as_float((uint32_t)p[k][v]), __uint_as_float((uint32_t)(p[k][v] >> 32)), in[v]);
+                    }
+        }
+        if (tile < tiles - 1)
+#pragma unroll
+            for (int v = 0; v < V; ++v) tell(work.out + at + 64 * v, told(through(A[v], H[v], in[v])));
+#pragma unroll
+        for (int v = 0; v < V; ++v) come[v][lane] = in[v];
+    }
+    __syncthreads();
+    float now[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) now[v] = come[v][lane];
+    for (int i = 0; i < w; ++i)
+#pragma unroll
+        for (int v = 0; v < V; ++v) now[v] = through(spans[i][v][lane].A, spans[i][v][lane].H, now[v]);
+    s.run(c, mine, now);
+    if (tile == tiles - 1 && w == kWaves - 1) c.outgoing(now);
+}
+
+__global__ __launch_bounds__(256) void gated_clear_kernel(u32x4 *p, long long n)
+{
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) p[i] = kClear;
+}
+
+// A few steps: a lane takes V channels through all of them.
+template <typename T, int V, bool VEC, bool BACK>
+__global__ __launch_bounds__(64) void gated_few_kernel(Gated a, int groups)
+{
+    const Chain<T, V, VEC, BACK> c(a, blockIdx.x, groups, threadIdx.x);
+    float v[V];
+    c.incoming(v);
+    Span<T, V, VEC, BACK, 4> s;
+    for (int s0 = 0; s0 < a.L; s0 += 4) {
+        s.read(c, s0);
+        float A[V], H[V];
+        s.gates(c, s0, A, H);
+        s.run(c, s0, v);
+    }
+    c.outgoing(v);
+}
+
+enum { kFew, kWalk, kTiles };
+struct Plan {
+    int how, groups, chains, tiles;
+    size_t bytes;
+};
+Plan plan(int B, int L, int D, bool is_bf16)
+{
+    const int V = is_bf16 ? 2 : 1;
+    Plan p = {};
+    p.groups = (D + 64 * V - 1) / (64 * V);
+    p.chains = (int)((long long)B * p.groups);
+    p.tiles = (L + kTile - 1) / kTile;
+    p.how = L <= 16 ? kFew : p.tiles == 1 || p.chains >= 4 * device_cu_count() ? kWalk : kTiles;
+    if (p.how == kTiles) p.bytes = 256 + (size_t)p.tiles * p.chains * (64 * V) * 12;
+    return p;
+}
+
+template <bool BACK> hipError_t launch(const Gated &a, bool is_bf16, bool aligned, hipStream_t stream)
+{
+    const Plan p = plan(a.B, a.L, a.D, is_bf16);
+    auto with = [&](auto one, auto vec) {
+        using T = decltype(one);
+        constexpr int V = sizeof(T) == 2 ? 2 : 1;
+        if (p.how == kFew) {
+            hipLaunchKernelGGL((gated_few_kernel<T, V, vec.value, BACK>), dim3(p.chains), dim3(64), 0, stream, a, p.groups);
+        } else if (p.how == kWalk) {
+            hipLaunchKernelGGL((gated_walk_kernel<T, V, vec.value, BACK>), dim3(p.chains), dim3(64 * kWaves), 0, stream, a, p.groups);
+        } else {
+            const long long n = (long long)((p.bytes + 15) / 16), blocks = (n + 255) / 256, most = 8LL * device_cu_count();
+            hipLaunchKernelGGL(gated_clear_kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, stream,
+                               static_cast<u32x4 *>(a.work), n);
+            const size_t words = (size_t)p.tiles * p.chains * (64 * V);
+            char *base = static_cast<char *>(a.work);
+            Work work;
+            work.next = reinterpret_cast<uint32_t *>(base);
+            work.span = reinterpret_cast<unsigned long long *>(base + 256);
+            work.out = reinterpret_cast<uint32_t *>(base + 256 + words * 8);
+            hipLaunchKernelGGL((gated_tile_kernel<T, V, vec.value, BACK>), dim3((unsigned)((long long)p.chains * p.tiles)),
+                               dim3(64 * kWaves), 0, stream, a, p.groups, p.chains, p.tiles, work);
+        }
+    };
+    if (is_bf16) {
+        if (aligned) with((bf16)0.f, std::true_type{});
+        else with((bf16)0.f, std::false_type{});
+    } else {
+        with(0.f, std::true_type{});
+    }
+    return hipGetLastError();
+}
+
+// whether V channels of a token lie in whole words everywhere (fp32 takes one at a time)
+inline bool words(const void *p, long long batch, long long token)
+{
+    return reinterpret_cast<uintptr_t>(p) % 4 == 0 && batch % 2 == 0 && token % 2 == 0;
 }
 
 }  // namespace
 
-size_t gated_workspace_bytes(int, int, int, bool) { return 0; }
+size_t gated_workspace_bytes(int B, int L, int D, bool is_bf16)
+{
+    const size_t n = plan(B, L, D, is_bf16).bytes;
+    return (n + 15) / 16 * 16;
+}
 
 hipError_t launch_gated_fwd(const Gated &a, bool is_bf16, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(a.B * (long long)((a.D + 63) / 64)));
-    if (is_bf16) hipLaunchKernelGGL(gated_fwd_kernel<bf16>, grid, dim3(64), 0, stream, a);
-    else hipLaunchKernelGGL(gated_fwd_kernel<float>, grid, dim3(64), 0, stream, a);
-    return hipGetLastError();
+    return launch<false>(a, is_bf16, a.D % 2 == 0 && words(a.X, a.xb, a.xt) && words(a.G, a.gb, a.gt), stream);
 }
 
 hipError_t launch_gated_bwd(const Gated &a, bool is_bf16, hipStream_t stream)
 {
-    const dim3 grid((unsigned)(a.B * (long long)((a.D + 63) / 64)));
-    if (is_bf16) hipLaunchKernelGGL(gated_bwd_kernel<bf16>, grid, dim3(64), 0, stream, a);
-    else hipLaunchKernelGGL(gated_bwd_kernel<float>, grid, dim3(64), 0, stream, a);
-    return hipGetLastError();
+    return launch<true>(a, is_bf16, a.D % 2 == 0 && (!a.X || words(a.X, a.xb, a.xt)) && words(a.G, a.gb, a.gt) && words(a.dY, a.dyb, a.dyt),
+                        stream);
 }
 
 }  // namespace pf
