@@ -132,23 +132,189 @@ __global__ __launch_bounds__(512) void matmul_rows_kernel(Matmul a)
     }
 }
 
+// Many rows of A: tiles of BM rows of A by BN of B, WM x WN wavefronts, blocks of K in LDS twice (one in use, one on its way
+// from memory, straight into LDS).  A row of a block is eight pieces of 16 bytes; piece p of a row lies at place p ^ key, so that
+// sixteen lanes that read the same piece of sixteen rows meet different banks: the key is what tells apart eight neighbouring
+// lanes of a read, the row's last three bits for A, and for B, whose lanes go over rows 16 (r >> 2) + (r & 3) so that a lane ends up with
+// 16 neighbouring columns of C, two bits from either part.
+template <int BM, int BN, int WM, int WN, bool EXACT, bool ROWS> struct Tile {
+    static constexpr int kThreads = 64 * WM * WN, MT = BM / WM / 16;
+    static_assert(BN / WN == 64, "a wavefront has 64 columns");
+    static constexpr int kA = BM * 128, kB = BN * 128, kBuffer = kA + kB + 4 * BM + (ROWS ? 4 * BN : 0);
+};
+
+// what lies behind `bytes` reads as zeros
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, uint32_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, 0x00020000);
+}
+__device__ __forceinline__ void to_lds16(__amdgpu_buffer_rsrc_t from, uint32_t at, void *l)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)l, 16, (int)at, 0, 0, 0);
+}
+__device__ __forceinline__ void to_lds4(const void *g, void *l)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)g, (__attribute__((address_space(3))) void *)l, 4, 0, 0);
+}
+
+template <typename TO, int BM, int BN, int WM, int WN, bool ROWS>
+__global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int tiles_m, int tiles_n)
+{
+    constexpr bool EXACT = sizeof(TO) == 4;
+    using S = Tile<BM, BN, WM, WN, EXACT, ROWS>;
+    constexpr int MT = S::MT, kRound = S::kThreads / 8;      // rows that one load of all threads brings
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int wm = w / WN, wn = w % WN;
+    const unsigned id = xcd_consecutive(blockIdx.x, tiles_m * tiles_n);
+    // tiles next to each other share rows of A or B: eight tiles down, then one to the right
+    const unsigned band = id / (8 * tiles_n), in_band = id % (8 * tiles_n), deep = min(8u, tiles_m - 8 * band);
+    const long long m0 = (long long)__builtin_amdgcn_readfirstlane(8 * band + in_band % deep) * BM;      // (unsigned division is
+    const long long n0 = (long long)__builtin_amdgcn_readfirstlane(in_band / deep) * BN;                 // done in the lanes)
+    const int nk = a.K / 128 + (a.K % 128 != 0), last = (a.K + 15) / 16 * 16 - 16;
+    const int rows_a = (int)min((long long)BM, a.M - m0), rows_b = (int)min((long long)BN, a.N - n0);
+    const uint32_t lda = (uint32_t)a.lda, ldb = (uint32_t)a.ldb;
+    const auto A = buffer_of(static_cast<const uint8_t *>(a.A) + m0 * a.lda, (rows_a - 1) * lda + last + 16);
+    const auto B = buffer_of(static_cast<const uint8_t *>(a.B) + n0 * a.ldb, (rows_b - 1) * ldb + last + 16);
+    const int row = threadIdx.x >> 3, place = threadIdx.x & 7;
+    const int piece_a = (place ^ (row & 7)) * 16, piece_b = (place ^ ((row & 3) | (row >> 2 & 4))) * 16;
+    const uint32_t at_a = row * lda + piece_a, at_b = row * ldb + piece_b;
+    auto fetch = [&](int kb, uint8_t *buf) {      // (behind a row's end: the next row's values, taken out below)
+#pragma unroll
+        for (int i = 0; i < BM / kRound; ++i) to_lds16(A, at_a + (kb * 128 + i * kRound * lda), buf + (i * kRound * 128 + w * 1024));
+#pragma unroll
+        for (int i = 0; i < BN / kRound; ++i) to_lds16(B, at_b + (kb * 128 + i * kRound * ldb), buf + S::kA + (i * kRound * 128 + w * 1024));
+        constexpr int waves = WM * WN;
+        const float *sa = a.sa + (long long)kb * a.M + m0, *sb = a.sb + (long long)kb * a.N + n0;
+#pragma unroll
+        for (int i = 0; i < (BM / 64 + waves - 1) / waves; ++i) {
+            const int part = i * waves + w;
+            if (part < BM / 64) to_lds4(sa + min(part * 64 + lane, rows_a - 1), buf + S::kA + S::kB + part * 256);
+        }
+        if constexpr (ROWS)
+#pragma unroll
+            for (int i = 0; i < (BN / 64 + waves - 1) / waves; ++i) {
+                const int part = i * waves + (waves - 1 - w);
+                if (part < BN / 64) to_lds4(sb + min(part * 64 + lane, rows_b - 1), buf + S::kA + S::kB + 4 * BM + part * 256);
+            }
+    };
+    f32x4 acc[MT][4];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+    const int from_a = (wm * (BM / WM) + r) * 128 + ((g ^ (r & 7)) * 16);
+    const int from_b = S::kA + (wn * 64 + 16 * (r >> 2) + (r & 3)) * 128 + ((g ^ (r & 7)) * 16);
+    const int nb = (a.N + 127) / 128;
+    const float *sb_at = a.sb + min((long long)(n0 + wn * 64) / 128, (long long)nb - 1);
+    auto step = [&](float sb1, const uint8_t *buf) {
+        auto part = [&](int at) {
+            Part<EXACT> p;
+            p.set(*reinterpret_cast<const u32x4 *>(buf + at), *reinterpret_cast<const u32x4 *>(buf + (at ^ 64)));
+            return p;
+        };
+        const float *sa = reinterpret_cast<const float *>(buf + S::kA + S::kB) + wm * (BM / WM) + r;
+        const f32x4 *sb = reinterpret_cast<const f32x4 *>(buf + S::kA + S::kB + 4 * BM + 4 * (wn * 64 + 16 * g));
+        Part<EXACT> b[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b[j] = part(from_b + j * 512);
+        // Parts of A one after the other (all at once would not fit the registers); the sums of one are scaled while the
+        // products of the next run.
+        Part<EXACT> p = part(from_a);
+        f32x4 c[2][4];
+        float s[2];
+#pragma unroll
+        for (int i = 0; i <= MT; ++i) {
+            if (i < MT) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) c[i % 2][j] = product(b[j], p);
+                s[i % 2] = sa[16 * i];
+                if (i + 1 < MT) p = part(from_a + (i + 1) * 2048);
+            }
+            if (i > 0) {
+                const int o = (i - 1) % 2;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if constexpr (ROWS) acc[i - 1][j] += c[o][j] * (sb[j] * s[o]);
+                    else acc[i - 1][j] += c[o][j] * (sb1 * s[o]);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // of squares, a wavefront's columns have one scale: it is on its way for a block too
+    auto square = [&](int kb) { return ROWS ? 0.f : sb_at[(long long)kb * nb]; };
+    float next = square(0);
+    fetch(0, lds);
+    for (int kb = 0; kb < nk; ++kb) {
+        __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): this wavefront's part of block kb is in LDS
+        __syncthreads();                         // and the others', and nobody reads the other buffer any more
+        uint8_t *buf = lds + kb % 2 * S::kBuffer;
+        const float now = next;
+        if (kb + 1 < nk) {
+            next = square(kb + 1);
+            fetch(kb + 1, lds + (kb + 1) % 2 * S::kBuffer);
+        } else if (a.K % 128) {      // every thread clears behind K what it has brought itself
+            const int left = a.K - kb * 128;
+#pragma unroll
+            for (int i = 0; i < (BM + BN) / kRound; ++i) {
+                const int k = i < BM / kRound ? piece_a : piece_b;
+                u32x4 *q = reinterpret_cast<u32x4 *>(buf + i * kRound * 128 + threadIdx.x * 16);
+                if (k + 16 > left) *q = keep(*q, left - k);
+            }
+            __syncthreads();
+        }
+        step(now, buf);
+    }
+    TO *C = static_cast<TO *>(a.C);
+    const long long col = n0 + wn * 64 + 16 * g;
+    const int left = (int)min(16LL, a.N - col);
+    const bool whole = left == 16 && (a.ldc * (long long)sizeof(TO)) % 16 == 0;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        const long long m = m0 + wm * (BM / WM) + 16 * i + r;
+        if (m >= a.M) continue;
+        TO *to = C + m * a.ldc + col;
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+            const f32x8 v = __builtin_shufflevector(acc[i][j], acc[i][j + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+            if (whole) store8<TO, true>(to + 4 * j, rounded<TO, true>(v), 8);
+            else store8<TO, false>(to + 4 * j, rounded<TO, false>(v), left - 4 * j);
+        }
+    }
+}
+
 }  // namespace
 
 size_t matmul_workspace_bytes(int, int, int, int) { return 0; }
 
 hipError_t launch_matmul(const Matmul &a, bool bf16_out, hipStream_t stream)
 {
+    hipError_t status = hipSuccess;
     auto launch = [&](auto one) {
         auto rows = [&](auto MT) {
             hipLaunchKernelGGL((matmul_rows_kernel<decltype(one), MT.value>),
                                dim3((a.N + 15) / 16, (unsigned)((a.M + 16LL * MT.value - 1) / (16 * MT.value))), dim3(512), 0, stream, a);
         };
-        if (a.M <= 16) rows(std::integral_constant<int, 1>{});
-        else rows(std::integral_constant<int, 4>{});
+        if (a.M <= 16) return rows(std::integral_constant<int, 1>{});
+        if (a.M <= 64 || a.lda > (1 << 23) || a.ldb > (1 << 23)) return rows(std::integral_constant<int, 4>{});
+        auto tile = [&](auto by_rows) {
+            constexpr int BM = sizeof(one) == 4 ? 128 : 256, BN = 256, WM = 2, WN = 4;
+            using S = Tile<BM, BN, WM, WN, sizeof(one) == 4, by_rows.value>;
+            auto kernel = matmul_tile_kernel<decltype(one), BM, BN, WM, WN, by_rows.value>;
+            static std::atomic<uint64_t> armed{0};
+            const size_t bytes = 2 * S::kBuffer;
+            status = arm_dynamic_lds(armed, reinterpret_cast<const void *>(kernel), bytes);
+            if (status != hipSuccess) return;
+            const int tm = (int)((a.M + (long long)BM - 1) / BM), tn = (int)((a.N + (long long)BN - 1) / BN);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)tm * (unsigned)tn), dim3(S::kThreads), bytes, stream, a, tm, tn);
+        };
+        if (a.b_rows == 1) tile(std::true_type{});
+        else tile(std::false_type{});
     };
     if (bf16_out) launch((bf16)0.f);
     else launch(0.f);
-    return hipGetLastError();
+    return status == hipSuccess ? hipGetLastError() : status;
 }
 
 }  // namespace pf
