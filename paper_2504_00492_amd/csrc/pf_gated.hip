@@ -2,7 +2,7 @@
 // the other way: with m = a_{t+1} l_{t+1} coming in, l_t = dy_t + m and a_t l_t goes out.
 //
 // A span of steps takes what comes in, v, to A v + H: A the product of its gates, H what it makes of zero.  Spans join as
-// (A, H) then (A', H') = (A' A, A' H + H'), so they can be read side by side.  A wavefront holds 64 V channels of kSteps
+// (A, H) then (A', H') = (A' A, A' H + H'), so they can be read side by side.  A wavefront holds 64 V channels of some
 // consecutive steps in registers, a workgroup kWaves such spans, one behind the other: a tile.  Each span's (A, H) is formed first, the
 // spans in front are put through it, and the steps run once more from what really comes in.  Memory sees every array once.
 //
@@ -17,26 +17,31 @@
 #include "pf_layer_common.h"
 #include "pf_layer_internal.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace pf {
 
 namespace {
 
-constexpr int kWaves = 8, kSteps = 16, kTile = kWaves * kSteps;
-constexpr int kBehind = 8;      // tiles in front that are looked at together
+constexpr int kWaves = 8, kWalkSteps = 16;
+// Steps of a wavefront's span of a tile: as many as the registers hold two workgroups to a compute unit of (forward two
+// arrays, backward four); longer tiles have fewer words to tell and to wait for (1 x 65536 x 4096, bf16: 16 steps 351 us,
+// 24 320).
+template <typename T, bool BACK> constexpr int kTileSteps = BACK ? 16 : sizeof(T) == 2 ? 24 : 32;
+template <typename T> inline int tile_tokens(bool back) { return kWaves * (back ? kTileSteps<T, true> : kTileSteps<T, false>); }
 
 // the decay a, 1 - a, and d a / d g of a gate's value
 struct Gate { float a, rest, slope; };
 __device__ __forceinline__ float exponential(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
-// form and mix are the same for a whole launch; what is not used of the result is not computed
-__device__ __forceinline__ Gate gate_of(float g, int form, bool mix)
+// what is not used of the result is not computed
+template <int FORM, bool MIX> __device__ __forceinline__ Gate gate_of(float g)
 {
-    if (form == 0) return {g, 1.f - g, 1.f};
-    if (form == 1) {
+    if (FORM == 0) return {g, 1.f - g, 1.f};
+    if (FORM == 1) {
         const float a = exponential(g);
         float rest = 0.f;
-        if (mix) {      // 1 - e^g: near zero the series, whose first term left out is 2e-8 of it
+        if (MIX) {      // 1 - e^g: near zero the series, whose first term left out is 2e-8 of it
             float p = 1.f / 5040;
             p = fmaf(p, g, 1.f / 720);
             p = fmaf(p, g, 1.f / 120);
@@ -48,7 +53,8 @@ __device__ __forceinline__ Gate gate_of(float g, int form, bool mix)
         }
         return {a, rest, a};
     }
-    const float e = exponential(-fabsf(g)), s = __builtin_amdgcn_rcpf(1.f + e), t = e * s;
+    const float e = exponential(-fabsf(g)), d = 1.f + e, near = __builtin_amdgcn_rcpf(d);
+    const float s = fmaf(fmaf(-d, near, 1.f), near, near), t = e * s;      // (one step of Newton: 1 / d but for the last rounding)
     return {g < 0.f ? t : s, g < 0.f ? s : t, t * s};
 }
 
@@ -57,6 +63,12 @@ __device__ __forceinline__ float through(float A, float H, float v) { return v =
 
 // V neighbouring channels of one token
 template <typename T, int V> struct Raw { uint32_t w[(sizeof(T) * V + 3) / 4]; };
+// the same value, but what was made of it before is made of it anew and not kept in registers until then
+template <typename T, int V> __device__ __forceinline__ void afresh(Raw<T, V> &r)
+{
+#pragma unroll
+    for (auto &w : r.w) asm volatile("" : "+v"(w));
+}
 template <typename T, int V, bool VEC> __device__ __forceinline__ Raw<T, V> fetch(const T *p, int left)
 {
     Raw<T, V> r = {};
@@ -106,6 +118,13 @@ struct Work {
 };
 
 // steps of a chain in the order of the recurrence: step s is token s, or of the backward token L - 1 - s
+// a call's kind: element type, channels a lane, whether these lie in whole words, direction, mix, and the gate's form
+template <typename T_, int V_, bool VEC_, bool BACK_, bool MIX_, int FORM_> struct Kind {
+    using T = T_;
+    static constexpr int V = V_, FORM = FORM_;
+    static constexpr bool VEC = VEC_, BACK = BACK_, MIX = MIX_;
+};
+
 template <typename T, int V, bool VEC, bool BACK> struct Chain {
     const Gated &a;
     const T *x, *g, *dy, *yin;      // (of the wavefront's first channel: the same for all lanes)
@@ -117,8 +136,9 @@ template <typename T, int V, bool VEC, bool BACK> struct Chain {
     unsigned mine;      // this lane's first
     __device__ __forceinline__ Chain(const Gated &a_, int chain, int groups, int lane) : a(a_)
     {
-        const long long b = chain / groups;
-        const int c = (chain % groups) * (64 * V);
+        const int sequence = __builtin_amdgcn_readfirstlane((unsigned)chain / (unsigned)groups);
+        const long long b = sequence;
+        const int c = (chain - sequence * groups) * (64 * V);
         mine = lane * V;
         left = a.D - c - (int)mine;
         const long long at = b * a.L * a.D + c;
@@ -152,21 +172,25 @@ template <typename T, int V, bool VEC, bool BACK> struct Chain {
     }
 };
 
-template <typename T, int V, bool VEC, bool BACK, int N> struct Span;
+template <typename K, int N, bool BACK = K::BACK> struct Span;
 
-// forward: N steps in registers
-template <typename T, int V, bool VEC, int N> struct Span<T, V, VEC, false, N> {
+// Forward: N steps in registers, as they lie in memory; the gates are kept between the two times they are needed, but with
+// the mix they are formed again (half the registers).
+template <typename K, int N> struct Span<K, N, false> {
+    using T = typename K::T;
+    static constexpr int V = K::V, FORM = K::FORM;
+    static constexpr bool VEC = K::VEC, MIX = K::MIX;
     using C = Chain<T, V, VEC, false>;
     Raw<T, V> x[N], g[N];
-    float a[N][V], b[N][V];
+    
     __device__ __forceinline__ void read(const C &c, int s0)
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const long long t = s0 + i;
             const int left = t < c.a.L ? c.left : 0;
-            x[i] = fetch<T, V, VEC>(c.x + t * c.a.xt + c.mine, left);
             g[i] = fetch<T, V, VEC>(c.g + t * c.a.gt + c.mine, left);
+            x[i] = fetch<T, V, VEC>(c.x + t * c.a.xt + c.mine, left);
         }
     }
     __device__ __forceinline__ void gates(const C &c, int s0, float (&A)[V], float (&H)[V])
@@ -177,28 +201,37 @@ template <typename T, int V, bool VEC, int N> struct Span<T, V, VEC, false, N> {
         for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Gate k = gate_of(value(g[i], v), c.a.gate, c.a.mix);
-                const float in = value(x[i], v);
-                a[i][v] = s0 + i < c.a.L ? k.a : 1.f;
-                b[i][v] = s0 + i < c.a.L ? (c.a.mix ? k.rest * in : in) : 0.f;
-                A[v] *= a[i][v];
-                H[v] = fmaf(a[i][v], H[v], b[i][v]);
+                const Gate k = gate_of<FORM, MIX>(value(g[i], v));
+                const float in = value(x[i], v), now = s0 + i < c.a.L ? k.a : 1.f;      // (behind the end x is zero)
+                A[v] *= now;
+                H[v] = fmaf(now, H[v], MIX ? k.rest * in : in);
+                if (v == V - 1 && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);      // (all gates side by side would not fit the registers)
             }
     }
     __device__ __forceinline__ void run(const C &c, int s0, float (&v)[V])
     {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
+            if (s0 + i >= c.a.L) break;
+            afresh(g[i]);
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = fmaf(a[i][j], v[j], b[i][j]);
-            if (s0 + i < c.a.L) keep<T, V, VEC>(c.o0 + (long long)(s0 + i) * c.a.D + c.mine, v, c.left);
+            for (int j = 0; j < V; ++j) {
+                const Gate k = gate_of<FORM, MIX>(value(g[i], j));
+                const float in = value(x[i], j);
+                v[j] = fmaf(k.a, v[j], MIX ? k.rest * in : in);
+            }
+            keep<T, V, VEC>(c.o0 + (long long)(s0 + i) * c.a.D + c.mine, v, c.left);
+            if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
         }
     }
 };
 
-template <typename T, int V, bool VEC, int N> struct Span<T, V, VEC, true, N> {
+template <typename K, int N> struct Span<K, N, true> {
+    using T = typename K::T;
+    static constexpr int V = K::V, FORM = K::FORM;
+    static constexpr bool VEC = K::VEC, MIX = K::MIX;
     using C = Chain<T, V, VEC, true>;
-    Raw<T, V> x[N], g[N], dy[N], y[N];
+    Raw<T, V> x[MIX ? N : 1], g[N], dy[N], y[N];
     __device__ __forceinline__ void read(const C &c, int s0)
     {
 #pragma unroll
@@ -208,7 +241,8 @@ template <typename T, int V, bool VEC, int N> struct Span<T, V, VEC, true, N> {
             g[i] = fetch<T, V, VEC>(c.g + t * c.a.gt + c.mine, left);
             dy[i] = fetch<T, V, VEC>(c.dy + t * c.a.dyt + c.mine, left);
             y[i] = fetch<T, V, VEC>(c.yin + (t - 1) * c.a.D + c.mine, t > 0 ? c.left : 0);
-            if (c.a.mix) x[i] = fetch<T, V, VEC>(c.x + t * c.a.xt + c.mine, left);
+            if (MIX) x[MIX ? i : 0] = fetch<T, V, VEC>(c.x + t * c.a.xt + c.mine, left);
+            if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);      // (the addresses of all rows would not fit the scalar registers)
         }
     }
     __device__ __forceinline__ void gates(const C &c, int s0, float (&A)[V], float (&H)[V])
@@ -219,9 +253,10 @@ template <typename T, int V, bool VEC, int N> struct Span<T, V, VEC, true, N> {
         for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float a = s0 + i < c.a.L ? gate_of(value(g[i], v), c.a.gate, false).a : 1.f;
+                const float a = s0 + i < c.a.L ? gate_of<FORM, false>(value(g[i], v)).a : 1.f;
                 A[v] *= a;
                 H[v] = a * (value(dy[i], v) + H[v]);
+                if (v == V - 1 && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
             }
     }
     __device__ __forceinline__ void run(const C &c, int s0, float (&v)[V])
@@ -230,19 +265,21 @@ template <typename T, int V, bool VEC, int N> struct Span<T, V, VEC, true, N> {
         for (int i = 0; i < N; ++i) {
             const long long t = (long long)c.a.L - 1 - s0 - i;
             if (t < 0) break;
+            afresh(g[i]);
             float dx[V], dg[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const Gate k = gate_of(value(g[i], j), c.a.gate, c.a.mix);
+                const Gate k = gate_of<FORM, MIX>(value(g[i], j));
                 const float l = value(dy[i], j) + v[j];
                 float h = t > 0 ? value(y[i], j) : c.a.h0 && j < c.left ? c.a.h0[c.state + j] : 0.f;
-                if (c.a.mix) h -= value(x[i], j);
-                dx[j] = c.a.mix ? k.rest * l : l;
+                if (MIX) h -= value(x[MIX ? i : 0], j);
+                dx[j] = MIX ? k.rest * l : l;
                 dg[j] = l * h * k.slope;
                 v[j] = k.a * l;
             }
             keep<T, V, VEC>(c.o0 + t * c.a.D + c.mine, dx, c.left);
             keep<T, V, VEC>(c.o1 + t * c.a.D + c.mine, dg, c.left);
+            if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
         }
     }
 };
@@ -250,17 +287,19 @@ template <typename T, int V, bool VEC, int N> struct Span<T, V, VEC, true, N> {
 struct Pair { float A, H; };
 
 // A workgroup for each chain, from tile to tile.
-template <typename T, int V, bool VEC, bool BACK>
-__global__ __launch_bounds__(64 * kWaves) void gated_walk_kernel(Gated a, int groups)
+template <typename K>
+__device__ __forceinline__ void gated_walk(const Gated &a, int groups, Pair (&spans)[2][kWaves][K::V][64])
 {
-    __shared__ Pair spans[2][kWaves][V][64];
+    using T = typename K::T;
+    constexpr int V = K::V;
+    constexpr bool VEC = K::VEC;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Chain<T, V, VEC, BACK> c(a, blockIdx.x, groups, lane);
+    const Chain<T, V, VEC, K::BACK> c(a, blockIdx.x, groups, lane);
     float in[V];
     c.incoming(in);
-    Span<T, V, VEC, BACK, kSteps> s;
-    for (int s0 = 0, turn = 0; s0 < a.L; s0 += kTile, turn ^= 1) {
-        const int mine = s0 + w * kSteps;
+    Span<K, kWalkSteps> s;
+    for (int s0 = 0, turn = 0; s0 < a.L; s0 += kWaves * kWalkSteps, turn ^= 1) {
+        const int mine = s0 + w * kWalkSteps;
         s.read(c, mine);
         float A[V], H[V];
         s.gates(c, mine, A, H);
@@ -278,101 +317,109 @@ __global__ __launch_bounds__(64 * kWaves) void gated_walk_kernel(Gated a, int gr
             }
         }
         s.run(c, mine, now);
-        if (s0 + kTile >= a.L && w == kWaves - 1) c.outgoing(now);
+        if (s0 + kWaves * kWalkSteps >= a.L && w == kWaves - 1) c.outgoing(now);
     }
 }
 
 // A workgroup for each tile.
-template <typename T, int V, bool VEC, bool BACK>
-__global__ __launch_bounds__(64 * kWaves) void gated_tile_kernel(Gated a, int groups, int chains, int tiles, Work work)
+template <int V> struct TileLds {
+    Pair spans[kWaves][V][64], behind[kWaves][V][64];
+    float outs[kWaves][V][64];
+    int heard[kWaves];      // of a tile in front: 1 its (A, H), 2 what goes out of it
+    uint32_t ticket;
+};
+template <typename K>
+__device__ __forceinline__ void gated_tile(const Gated &a, int groups, int chains, int tiles, const Work &work, TileLds<K::V> &lds)
 {
-    __shared__ Pair spans[kWaves][V][64];
-    __shared__ float come[V][64];
-    __shared__ uint32_t ticket;
+    using T = typename K::T;
+    constexpr int V = K::V;
+    constexpr bool VEC = K::VEC;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (threadIdx.x == 0) ticket = __hip_atomic_fetch_add(work.next, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u;
-    __syncthreads();
-    const uint32_t id = __builtin_amdgcn_readfirstlane(ticket);
-    const int tile = id / chains, chain = id % chains, s0 = tile * kTile, mine = s0 + w * kSteps;
-    const Chain<T, V, VEC, BACK> c(a, chain, groups, lane);
-    Span<T, V, VEC, BACK, kSteps> s;
+    const uint32_t id = __builtin_amdgcn_readfirstlane(lds.ticket);
+    const int tile = __builtin_amdgcn_readfirstlane(id / chains), chain = (int)id - tile * chains;      // (unsigned division is done in the lanes)
+    constexpr int steps = kTileSteps<T, K::BACK>;
+    const int mine = (tile * kWaves + w) * steps;
+    const Chain<T, V, VEC, K::BACK> c(a, chain, groups, lane);
+    Span<K, steps> s;
     s.read(c, mine);
     float A[V], H[V];
     s.gates(c, mine, A, H);
 #pragma unroll
-    for (int v = 0; v < V; ++v) spans[w][v][lane] = {A[v], H[v]};
+    for (int v = 0; v < V; ++v) lds.spans[w][v][lane] = {A[v], H[v]};
     __syncthreads();
-    if (w == 0) {
-        // words of a tile of this chain lie side by side: [tile][chain][v][lane]
-        const long long row = (long long)chains * (64 * V), at = (long long)tile * row + (long long)chain * (64 * V) + lane;
+    // words of a tile of this chain lie side by side: [tile][chain][v][lane]
+    const long long row = (long long)chains * (64 * V), at = (long long)tile * row + (long long)chain * (64 * V);
+    if (w == 0 && tile < tiles - 1) {
 #pragma unroll
         for (int i = 1; i < kWaves; ++i)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Pair p = spans[i][v][lane];
+                const Pair p = lds.spans[i][v][lane];
                 A[v] *= p.A;
                 H[v] = fmaf(p.A, H[v], p.H);
             }
-        float in[V];
-        if (tile == 0) {
-            c.incoming(in);
-        } else {
-            if (tile < tiles - 1)
+        if (tile > 0)
 #pragma unroll
-                for (int v = 0; v < V; ++v)
-                    tell(work.span + at + 64 * v, (unsigned long long)told(H[v]) << 32 | told(A[v]));
-            int from;      // the nearest tile that has told for all of this wavefront's channels
-            while (true) {
-                uint32_t o[kBehind][V];
-#pragma unroll
-                for (int k = 0; k < kBehind; ++k)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) o[k][v] = hear(work.out + at + 64 * v - (long long)min(k + 1, tile) * row);
-                from = -1;
-#pragma unroll
-                for (int k = kBehind - 1; k >= 0; --k) {
-                    bool ready = k < tile;
-#pragma unroll
-                    for (int v = 0; v < V; ++v) ready = ready && o[k][v] != kClear;
-                    if (__all(ready)) {
-                        from = k;
-#pragma unroll
-                        for (int v = 0; v < V; ++v) in[v] = __uint_as_float(o[k][v]);
-                    }
-                }
-                if (from >= 0) break;
-                __builtin_amdgcn_s_sleep(1);
-            }
-            unsigned long long p[kBehind - 1][V];
-#pragma unroll
-            for (int k = 0; k < kBehind - 1; ++k)
-                if (k < from)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) p[k][v] = hear(work.span + at + 64 * v - (k + 1) * row);
-#pragma unroll
-            for (int k = kBehind - 2; k >= 0; --k)
-                if (k < from)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        while ((uint32_t)p[k][v] == kClear) p[k][v] = hear(work.span + at + 64 * v - (k + 1) * row);
-                        in[v] = through(__uint_as_float((uint32_t)p[k][v]), __uint_as_float((uint32_t)(p[k][v] >> 32)), in[v]);
-                    }
-        }
-        if (tile < tiles - 1)
-#pragma unroll
-            for (int v = 0; v < V; ++v) tell(work.out + at + 64 * v, told(through(A[v], H[v], in[v])));
-#pragma unroll
-        for (int v = 0; v < V; ++v) come[v][lane] = in[v];
+            for (int v = 0; v < V; ++v) tell(work.span + at + 64 * v + (unsigned)lane, (unsigned long long)told(H[v]) << 32 | told(A[v]));
     }
-    __syncthreads();
-    float now[V];
+    float in[V];
+    if (tile == 0) {
+        c.incoming(in);
+    } else {      // each wavefront listens to one of the tiles in front
+        const long long there = at - (long long)min(w + 1, tile) * row;
+        bool has_out = false, has_span = false;
+        int from;
+        while (true) {
+            if (!has_span && w < tile - 1) {      // (the first tile only tells what goes out)
+                bool ready = true;
 #pragma unroll
-    for (int v = 0; v < V; ++v) now[v] = come[v][lane];
+                for (int v = 0; v < V; ++v) {
+                    const unsigned long long p = hear(work.span + there + 64 * v + (unsigned)lane);
+                    ready = ready && (uint32_t)p != kClear;
+                    lds.behind[w][v][lane] = {__uint_as_float((uint32_t)p), __uint_as_float((uint32_t)(p >> 32))};
+                }
+                has_span = __all(ready);
+            }
+            if (!has_out && w < tile) {
+                bool ready = true;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const uint32_t o = hear(work.out + there + 64 * v + (unsigned)lane);
+                    ready = ready && o != kClear;
+                    lds.outs[w][v][lane] = __uint_as_float(o);
+                }
+                has_out = __all(ready);
+            }
+            if (lane == 0) lds.heard[w] = (has_span ? 1 : 0) | (has_out ? 2 : 0);
+            __syncthreads();
+            from = -1;      // the nearest tile whose outgoing values are told, if all between have told their (A, H)
+            bool open = true;
+#pragma unroll
+            for (int k = 0; k < kWaves; ++k) {
+                const int h = lds.heard[k];
+                if (open && (h & 2)) from = k, open = false;
+                open = open && (h & 1);
+            }
+            from = __builtin_amdgcn_readfirstlane(from);
+            if (from >= 0) break;
+            __syncthreads();
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) in[v] = lds.outs[from][v][lane];
+#pragma unroll 1
+        for (int k = from - 1; k >= 0; --k)
+#pragma unroll
+            for (int v = 0; v < V; ++v) in[v] = through(lds.behind[k][v][lane].A, lds.behind[k][v][lane].H, in[v]);
+    }
+    if (w == 0 && tile < tiles - 1)
+#pragma unroll
+        for (int v = 0; v < V; ++v) tell(work.out + at + 64 * v + (unsigned)lane, told(through(A[v], H[v], in[v])));
+#pragma unroll 1
     for (int i = 0; i < w; ++i)
 #pragma unroll
-        for (int v = 0; v < V; ++v) now[v] = through(spans[i][v][lane].A, spans[i][v][lane].H, now[v]);
-    s.run(c, mine, now);
-    if (tile == tiles - 1 && w == kWaves - 1) c.outgoing(now);
+        for (int v = 0; v < V; ++v) in[v] = through(lds.spans[i][v][lane].A, lds.spans[i][v][lane].H, in[v]);
+    s.run(c, mine, in);
+    if (tile == tiles - 1 && w == kWaves - 1) c.outgoing(in);
 }
 
 __global__ __launch_bounds__(256) void gated_clear_kernel(u32x4 *p, long long n)
@@ -381,13 +428,16 @@ __global__ __launch_bounds__(256) void gated_clear_kernel(u32x4 *p, long long n)
 }
 
 // A few steps: a lane takes V channels through all of them.
-template <typename T, int V, bool VEC, bool BACK>
-__global__ __launch_bounds__(64) void gated_few_kernel(Gated a, int groups)
+template <typename K>
+__device__ __forceinline__ void gated_few(const Gated &a, int groups)
 {
-    const Chain<T, V, VEC, BACK> c(a, blockIdx.x, groups, threadIdx.x);
+    using T = typename K::T;
+    constexpr int V = K::V;
+    constexpr bool VEC = K::VEC;
+    const Chain<T, V, VEC, K::BACK> c(a, blockIdx.x, groups, threadIdx.x);
     float v[V];
     c.incoming(v);
-    Span<T, V, VEC, BACK, 4> s;
+    Span<K, 4> s;
     for (int s0 = 0; s0 < a.L; s0 += 4) {
         s.read(c, s0);
         float A[V], H[V];
@@ -397,33 +447,63 @@ __global__ __launch_bounds__(64) void gated_few_kernel(Gated a, int groups)
     c.outgoing(v);
 }
 
+// The gate's form is asked once, not at every step: a body for each.
+template <typename T, int V, bool VEC, bool BACK, bool MIX, typename F> __device__ __forceinline__ void by_form(int gate, F f)
+{
+    if (gate == 0) f(Kind<T, V, VEC, BACK, MIX, 0>{});
+    else if (gate == 1) f(Kind<T, V, VEC, BACK, MIX, 1>{});
+    else f(Kind<T, V, VEC, BACK, MIX, 2>{});
+}
+template <typename T, int V, bool VEC, bool BACK, bool MIX>
+__global__ __launch_bounds__(64 * kWaves) void gated_walk_kernel(Gated a, int groups)
+{
+    __shared__ Pair spans[2][kWaves][V][64];
+    by_form<T, V, VEC, BACK, MIX>(a.gate, [&](auto k) { gated_walk<decltype(k)>(a, groups, spans); });
+}
+// (four wavefronts to a SIMD: two workgroups to a compute unit, so that one reads while the other waits; where channels lie at
+// odd places their registers allow three)
+template <typename T, int V, bool VEC, bool BACK, bool MIX>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(VEC ? 4 : 3)))
+void gated_tile_kernel(Gated a, int groups, int chains, int tiles, Work work)
+{
+    __shared__ TileLds<V> lds;
+    if (threadIdx.x == 0) lds.ticket = __hip_atomic_fetch_add(work.next, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u;
+    __syncthreads();
+    by_form<T, V, VEC, BACK, MIX>(a.gate, [&](auto k) { gated_tile<decltype(k)>(a, groups, chains, tiles, work, lds); });
+}
+template <typename T, int V, bool VEC, bool BACK, bool MIX> __global__ __launch_bounds__(64) void gated_few_kernel(Gated a, int groups)
+{
+    by_form<T, V, VEC, BACK, MIX>(a.gate, [&](auto k) { gated_few<decltype(k)>(a, groups); });
+}
+
 enum { kFew, kWalk, kTiles };
 struct Plan {
     int how, groups, chains, tiles;
     size_t bytes;
 };
-Plan plan(int B, int L, int D, bool is_bf16)
+Plan plan(int B, int L, int D, bool is_bf16, bool back)
 {
     const int V = is_bf16 ? 2 : 1;
     Plan p = {};
     p.groups = (D + 64 * V - 1) / (64 * V);
     p.chains = (int)((long long)B * p.groups);
-    p.tiles = (L + kTile - 1) / kTile;
-    p.how = L <= 16 ? kFew : p.tiles == 1 || p.chains >= 4 * device_cu_count() ? kWalk : kTiles;
+    const int tile = is_bf16 ? tile_tokens<bf16>(back) : tile_tokens<float>(back);
+    p.tiles = L / tile + (L % tile != 0);
+    p.how = L <= 16 ? kFew : L <= 2 * kWaves * kWalkSteps || p.chains >= 4 * device_cu_count() ? kWalk : kTiles;
     if (p.how == kTiles) p.bytes = 256 + (size_t)p.tiles * p.chains * (64 * V) * 12;
     return p;
 }
 
 template <bool BACK> hipError_t launch(const Gated &a, bool is_bf16, bool aligned, hipStream_t stream)
 {
-    const Plan p = plan(a.B, a.L, a.D, is_bf16);
-    auto with = [&](auto one, auto vec) {
+    const Plan p = plan(a.B, a.L, a.D, is_bf16, BACK);
+    auto with_mix = [&](auto one, auto vec, auto mix) {
         using T = decltype(one);
         constexpr int V = sizeof(T) == 2 ? 2 : 1;
         if (p.how == kFew) {
-            hipLaunchKernelGGL((gated_few_kernel<T, V, vec.value, BACK>), dim3(p.chains), dim3(64), 0, stream, a, p.groups);
+            hipLaunchKernelGGL((gated_few_kernel<T, V, vec.value, BACK, mix.value>), dim3(p.chains), dim3(64), 0, stream, a, p.groups);
         } else if (p.how == kWalk) {
-            hipLaunchKernelGGL((gated_walk_kernel<T, V, vec.value, BACK>), dim3(p.chains), dim3(64 * kWaves), 0, stream, a, p.groups);
+            hipLaunchKernelGGL((gated_walk_kernel<T, V, vec.value, BACK, mix.value>), dim3(p.chains), dim3(64 * kWaves), 0, stream, a, p.groups);
         } else {
             const long long n = (long long)((p.bytes + 15) / 16), blocks = (n + 255) / 256, most = 8LL * device_cu_count();
             hipLaunchKernelGGL(gated_clear_kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, stream,
@@ -434,9 +514,14 @@ template <bool BACK> hipError_t launch(const Gated &a, bool is_bf16, bool aligne
             work.next = reinterpret_cast<uint32_t *>(base);
             work.span = reinterpret_cast<unsigned long long *>(base + 256);
             work.out = reinterpret_cast<uint32_t *>(base + 256 + words * 8);
-            hipLaunchKernelGGL((gated_tile_kernel<T, V, vec.value, BACK>), dim3((unsigned)((long long)p.chains * p.tiles)),
+            const long long count = (long long)p.chains * p.tiles;
+            hipLaunchKernelGGL((gated_tile_kernel<T, V, vec.value, BACK, mix.value>), dim3((unsigned)count),
                                dim3(64 * kWaves), 0, stream, a, p.groups, p.chains, p.tiles, work);
         }
+    };
+    auto with = [&](auto one, auto vec) {
+        if (a.mix) with_mix(one, vec, std::true_type{});
+        else with_mix(one, vec, std::false_type{});
     };
     if (is_bf16) {
         if (aligned) with((bf16)0.f, std::true_type{});
@@ -457,7 +542,7 @@ inline bool words(const void *p, long long batch, long long token)
 
 size_t gated_workspace_bytes(int B, int L, int D, bool is_bf16)
 {
-    const size_t n = plan(B, L, D, is_bf16).bytes;
+    const size_t n = std::max(plan(B, L, D, is_bf16, false).bytes, plan(B, L, D, is_bf16, true).bytes);
     return (n + 15) / 16 * 16;
 }
 
