@@ -207,65 +207,97 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int
     const int from_b = S::kA + (wn * 64 + 16 * (r >> 2) + (r & 3)) * 128 + ((g ^ (r & 7)) * 16);
     const int nb = (a.N + 127) / 128;
     const float *sb_at = a.sb + min((long long)(n0 + wn * 64) / 128, (long long)nb - 1);
-    auto step = [&](float sb1, const uint8_t *buf) {
-        auto part = [&](int at) {
-            Part<EXACT> p;
-            p.set(*reinterpret_cast<const u32x4 *>(buf + at), *reinterpret_cast<const u32x4 *>(buf + (at ^ 64)));
-            return p;
-        };
-        const float *sa = reinterpret_cast<const float *>(buf + S::kA + S::kB) + wm * (BM / WM) + r;
-        const f32x4 *sb = reinterpret_cast<const f32x4 *>(buf + S::kA + S::kB + 4 * BM + 4 * (wn * 64 + 16 * g));
-        Part<EXACT> b[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) b[j] = part(from_b + j * 512);
-        // Parts of A one after the other (all at once would not fit the registers); the sums of one are scaled while the
-        // products of the next run.
-        Part<EXACT> p = part(from_a);
-        f32x4 c[2][4];
-        float s[2];
-#pragma unroll
-        for (int i = 0; i <= MT; ++i) {
-            if (i < MT) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) c[i % 2][j] = product(b[j], p);
-                s[i % 2] = sa[16 * i];
-                if (i + 1 < MT) p = part(from_a + (i + 1) * 2048);
-            }
-            if (i > 0) {
-                const int o = (i - 1) % 2;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if constexpr (ROWS) acc[i - 1][j] += c[o][j] * (sb[j] * s[o]);
-                    else acc[i - 1][j] += c[o][j] * (sb1 * s[o]);
-                }
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
+    auto part = [&](const uint8_t *buf, int at) {
+        Part<EXACT> p;
+        p.set(*reinterpret_cast<const u32x4 *>(buf + at), *reinterpret_cast<const u32x4 *>(buf + (at ^ 64)));
+        return p;
     };
-    // of squares, a wavefront's columns have one scale: it is on its way for a block too
-    auto square = [&](int kb) { return ROWS ? 0.f : sb_at[(long long)kb * nb]; };
-    float next = square(0);
-    fetch(0, lds);
-    for (int kb = 0; kb < nk; ++kb) {
-        __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): this wavefront's part of block kb is in LDS
-        __syncthreads();                         // and the others', and nobody reads the other buffer any more
-        uint8_t *buf = lds + kb % 2 * S::kBuffer;
-        const float now = next;
-        if (kb + 1 < nk) {
-            next = square(kb + 1);
-            fetch(kb + 1, lds + (kb + 1) % 2 * S::kBuffer);
-        } else if (a.K % 128) {      // every thread clears behind K what it has brought itself
+    auto buffer = [&](int kb) { return lds + kb % 2 * S::kBuffer; };
+    // block kb is in LDS for all wavefronts, and nobody reads the block before it any more
+    auto arrive = [&](int kb) {
+        __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): what this wavefront asked for is there
+        if (kb == nk - 1 && a.K % 128) {         // every thread clears behind K what it has brought itself
             const int left = a.K - kb * 128;
 #pragma unroll
             for (int i = 0; i < (BM + BN) / kRound; ++i) {
                 const int k = i < BM / kRound ? piece_a : piece_b;
-                u32x4 *q = reinterpret_cast<u32x4 *>(buf + i * kRound * 128 + threadIdx.x * 16);
+                u32x4 *q = reinterpret_cast<u32x4 *>(buffer(kb) + i * kRound * 128 + threadIdx.x * 16);
                 if (k + 16 > left) *q = keep(*q, left - k);
             }
-            __syncthreads();
         }
-        step(now, buf);
-    }
+        __syncthreads();
+    };
+    // of squares, a wavefront's columns have one scale a block, read by the scalar unit: a vector load between the blocks on their way
+    // to LDS would be waited for with them
+    auto square = [&](int kb) { return ROWS ? 0.f : ((const __attribute__((address_space(4))) float *)sb_at)[(long long)kb * nb]; };
+    float next = square(0);
+    fetch(0, buffer(0));
+    arrive(0);
+    if (nk > 1) fetch(1, buffer(1));
+    Part<EXACT> b[4], p[2];
+    float scale[MT];      // of the rows of A
+    auto scales = [&](const uint8_t *buf) {
+        const float *sa = reinterpret_cast<const float *>(buf + S::kA + S::kB) + wm * (BM / WM) + r;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) scale[i] = sa[16 * i];
+    };
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = part(buffer(0), from_b + j * 512);
+    p[0] = part(buffer(0), from_a);
+    scales(buffer(0));
+    auto block = [&](int kb, auto final) {
+        const uint8_t *buf = buffer(kb), *then = buffer(kb + 1);
+        f32x4 sb[4];
+        if constexpr (ROWS)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                sb[j] = reinterpret_cast<const f32x4 *>(buf + S::kA + S::kB + 4 * BM + 4 * (wn * 64 + 16 * g))[j];
+        // Parts of A one after the other (all at once would not fit the registers), two products at a time, whose sums are
+        // scaled while the next two run.  Before the last part the next block is waited for, so that its first parts are
+        // read while the last products run.
+        f32x4 c[2][2];
+        const float now = next;
+        if constexpr (!final.value) next = square(kb + 1);
+        auto add = [&](int h) {
+            const int i = h / 2;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                f32x4 &to = acc[i][h % 2 * 2 + j];
+                if constexpr (ROWS) to += c[h % 2][j] * (sb[h % 2 * 2 + j] * scale[i]);
+                else to += c[h % 2][j] * (now * scale[i]);
+                asm volatile("" : "+v"(to));      // (here, not behind the next branch, where the compiler would have it)
+            }
+        };
+#pragma unroll
+        for (int h = 0; h < 2 * MT; ++h) {
+            const int i = h / 2;
+            if (h % 2 == 0 && i + 1 < MT) p[(i + 1) % 2] = part(buf, from_a + (i + 1) * 2048);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) c[h % 2][j] = product(b[h % 2 * 2 + j], p[i % 2]);
+            if (h > 0) add(h - 1);
+            if (!final.value && h >= 2 * MT - 2)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) b[h % 2 * 2 + j] = part(then, from_b + (h % 2 * 2 + j) * 512);
+            if (!final.value && h == 2 * MT - 1) p[MT % 2] = part(then, from_a);
+            if constexpr (!EXACT) {
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+                __builtin_amdgcn_sched_group_barrier(0x2, 5, 0);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x2, 5, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (!final.value && h == 2 * MT - 3) arrive(kb + 1);
+        }
+        add(2 * MT - 1);
+        if constexpr (!final.value) {
+            scales(then);
+            if (kb + 2 < nk) fetch(kb + 2, buffer(kb));
+        }
+    };
+    static_assert(MT % 2 == 0, "parts of A in turn");
+    for (int kb = 0; kb + 1 < nk; ++kb) block(kb, std::false_type{});
+    block(nk - 1, std::true_type{});
     TO *C = static_cast<TO *>(a.C);
     const long long col = n0 + wn * 64 + 16 * g;
     const int left = (int)min(16LL, a.N - col);
