@@ -45,6 +45,7 @@ struct Matmul {
     float *part;
     long long lda, ldb, ldc;
     int M, N, K, b_rows;
+    long long sb_ld;      // of the scales of B: set by launch_matmul
 };
 size_t matmul_workspace_bytes(int M, int N, int K, int b_rows);
 hipError_t launch_matmul(const Matmul &a, bool bf16_out, hipStream_t stream);

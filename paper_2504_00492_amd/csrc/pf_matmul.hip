@@ -12,6 +12,7 @@
 #include "pf_layer_common.h"
 #include "pf_layer_internal.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace pf {
@@ -73,49 +74,70 @@ __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(bf16 *p, float v) { *p = (bf16)v; }
 
 // Few rows of A: the weights are what is read, once, straight into registers.  A workgroup takes 16 rows of B and 16 MT of
-// A; its eight wavefronts share the blocks of K between them and join their sums at the end, in their order.
-template <typename TO, int MT>      // (TO: float is also what asks for exact products)
-__global__ __launch_bounds__(512) void matmul_rows_kernel(Matmul a)
+// A; its eight wavefronts share the blocks of K between them, each with what U of them need on its way at once, and join
+// their sums at the end, in their order.
+template <typename TO, int MT, int U, bool ROWS>      // (TO: float is also what asks for exact products)
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) void matmul_rows_kernel(Matmul a)
 {
     __shared__ f32x4 sums[8][MT][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const long long n0 = (long long)blockIdx.x * 16, m0 = (long long)blockIdx.y * (16 * MT);
     const int nk = a.K / 128 + (a.K % 128 != 0), last = (a.K + 15) / 16 * 16 - 16;
-    const long long sb_ld = a.b_rows == 1 ? a.N : (a.N + 127LL) / 128;
     const uint8_t *B = static_cast<const uint8_t *>(a.B) + min(n0 + r, (long long)a.N - 1) * a.ldb;
     const uint8_t *A[MT];
     long long m[MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-        m[i] = min(m0 + 16 * i + r, (long long)a.M - 1);
+        m[i] = m0 + 16 * i + r;
         A[i] = static_cast<const uint8_t *>(a.A) + m[i] * a.lda;
     }
+    const long long sb_at = min(n0 + 4 * g, (long long)a.N - 1);      // of squares, 16 rows have one scale, read by the scalar unit
+    const auto *squares = (const __attribute__((address_space(4))) float *)(a.sb + n0 / 128);
     f32x4 acc[MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i) acc[i] = 0.f;
-    auto load = [&](const uint8_t *p, int kb, bool cut) {
-        const int k0 = kb * 128 + 16 * g, k1 = k0 + 64;
-        u32x4 lo = *reinterpret_cast<const u32x4 *>(p + min(k0, last)), hi = *reinterpret_cast<const u32x4 *>(p + min(k1, last));
-        if (cut) lo = keep(lo, a.K - k0), hi = keep(hi, a.K - k1);
+    struct Pieces { u32x4 lo, hi; };
+    auto load = [&](const uint8_t *p, int kb) {
+        const int k0 = kb * 128 + 16 * g;
+        return Pieces{*reinterpret_cast<const u32x4 *>(p + min(k0, last)), *reinterpret_cast<const u32x4 *>(p + min(k0 + 64, last))};
+    };
+    auto whole = [&](Pieces q, int kb) {      // what lies behind K counts as zeros
+        const int left = a.K - kb * 128 - 16 * g;
+        if (kb * 128 + 128 > a.K) q.lo = keep(q.lo, left), q.hi = keep(q.hi, left - 64);
         Part<sizeof(TO) == 4> part;
-        part.set(lo, hi);
+        part.set(q.lo, q.hi);
         return part;
     };
-    auto step = [&](int kb, bool cut) {
-        const auto b = load(B, kb, cut);
-        f32x4 sb;
+    for (int first = w; first < nk; first += 8 * U) {
+        Pieces b[U], p[U][MT];
+        f32x4 sb[U];
+        float sa[U][MT];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const long long n = min(n0 + 4 * g + e, (long long)a.N - 1);
-            sb[e] = a.sb[kb * sb_ld + (a.b_rows == 1 ? n : n / 128)];
+        for (int u = 0; u < U; ++u) {
+            const int kb = min(first + 8 * u, nk - 1);
+            b[u] = load(B, kb);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {      // (lanes of rows that A lacks ask for nothing)
+                p[u][i] = {};
+                sa[u][i] = 0.f;
+                if (m[i] < a.M) p[u][i] = load(A[i], kb), sa[u][i] = a.sa[(long long)kb * a.M + m[i]];
+            }
+            if constexpr (!ROWS) {
+                sb[u] = squares[kb * a.sb_ld];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sb[u][e] = a.sb[kb * a.sb_ld + min(sb_at + e, (long long)a.N - 1)];
+            }
         }
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const f32x4 p = product(b, load(A[i], kb, cut));
-            acc[i] += p * (sb * a.sa[(long long)kb * a.M + m[i]]);
+        for (int u = 0; u < U; ++u) {
+            const int kb = first + 8 * u;
+            if (kb >= nk) break;
+            const auto part = whole(b[u], kb);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) acc[i] += product(part, whole(p[u][i], kb)) * (sb[u] * sa[u][i]);
         }
-    };
-    for (int kb = w; kb < nk; kb += 8) step(kb, kb * 128 + 128 > a.K);
+    }
 #pragma unroll
     for (int i = 0; i < MT; ++i) sums[w][i][lane] = acc[i];
     __syncthreads();
@@ -132,14 +154,14 @@ __global__ __launch_bounds__(512) void matmul_rows_kernel(Matmul a)
     }
 }
 
-// Many rows of A: tiles of BM rows of A by BN of B, WM x WN wavefronts, blocks of K in LDS twice (one in use, one on its way
-// from memory, straight into LDS).  A row of a block is eight pieces of 16 bytes; piece p of a row lies at place p ^ key, so that
+// Many rows of A: tiles of BM rows of A by BN of B, WM x WN wavefronts, two blocks of K in LDS (one in use, one on its way
+// from memory, straight into LDS; more of them gave nothing).  A row of a block is eight pieces of 16 bytes; piece p of a row lies at place p ^ key, so that
 // sixteen lanes that read the same piece of sixteen rows meet different banks: the key is what tells apart eight neighbouring
 // lanes of a read, the row's last three bits for A, and for B, whose lanes go over rows 16 (r >> 2) + (r & 3) so that a lane ends up with
 // 16 neighbouring columns of C, two bits from either part.
-template <int BM, int BN, int WM, int WN, bool EXACT, bool ROWS> struct Tile {
+template <int BM, int BN, int WM, int WN, bool ROWS> struct Tile {
     static constexpr int kThreads = 64 * WM * WN, MT = BM / WM / 16;
-    static_assert(BN / WN == 64, "a wavefront has 64 columns");
+    static_assert(BN / WN == 64 && kThreads >= 256 && MT % 2 == 0, "a wavefront has 64 columns, a load 32 rows, parts of A take turns");
     static constexpr int kA = BM * 128, kB = BN * 128, kBuffer = kA + kB + 4 * BM + (ROWS ? 4 * BN : 0);
 };
 
@@ -157,21 +179,24 @@ __device__ __forceinline__ void to_lds4(const void *g, void *l)
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)g, (__attribute__((address_space(3))) void *)l, 4, 0, 0);
 }
 
+// splits > 1: each of so many workgroups of a tile takes a part of K and leaves its sums in a.part, [split][M][N].
 template <typename TO, int BM, int BN, int WM, int WN, bool ROWS>
-__global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int tiles_m, int tiles_n)
+__global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int tiles_m, int tiles_n, int splits)
 {
     constexpr bool EXACT = sizeof(TO) == 4;
-    using S = Tile<BM, BN, WM, WN, EXACT, ROWS>;
+    using S = Tile<BM, BN, WM, WN, ROWS>;
     constexpr int MT = S::MT, kRound = S::kThreads / 8;      // rows that one load of all threads brings
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int wm = w / WN, wn = w % WN;
-    const unsigned id = xcd_consecutive(blockIdx.x, tiles_m * tiles_n);
+    const unsigned place_of = xcd_consecutive(blockIdx.x, tiles_m * tiles_n * splits);
+    const unsigned id = place_of % (tiles_m * tiles_n), split = __builtin_amdgcn_readfirstlane(place_of / (tiles_m * tiles_n));
     // tiles next to each other share rows of A or B: eight tiles down, then one to the right
     const unsigned band = id / (8 * tiles_n), in_band = id % (8 * tiles_n), deep = min(8u, tiles_m - 8 * band);
     const long long m0 = (long long)__builtin_amdgcn_readfirstlane(8 * band + in_band % deep) * BM;      // (unsigned division is
     const long long n0 = (long long)__builtin_amdgcn_readfirstlane(in_band / deep) * BN;                 // done in the lanes)
-    const int nk = a.K / 128 + (a.K % 128 != 0), last = (a.K + 15) / 16 * 16 - 16;
+    const int blocks = a.K / 128 + (a.K % 128 != 0), last = (a.K + 15) / 16 * 16 - 16;
+    const int k0 = (int)((long long)blocks * split / splits), nk = (int)((long long)blocks * (split + 1) / splits);      // this split's
     const int rows_a = (int)min((long long)BM, a.M - m0), rows_b = (int)min((long long)BN, a.N - n0);
     const uint32_t lda = (uint32_t)a.lda, ldb = (uint32_t)a.ldb;
     const auto A = buffer_of(static_cast<const uint8_t *>(a.A) + m0 * a.lda, (rows_a - 1) * lda + last + 16);
@@ -184,8 +209,8 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int
         for (int i = 0; i < BM / kRound; ++i) to_lds16(A, at_a + (kb * 128 + i * kRound * lda), buf + (i * kRound * 128 + w * 1024));
 #pragma unroll
         for (int i = 0; i < BN / kRound; ++i) to_lds16(B, at_b + (kb * 128 + i * kRound * ldb), buf + S::kA + (i * kRound * 128 + w * 1024));
-        constexpr int waves = WM * WN;
-        const float *sa = a.sa + (long long)kb * a.M + m0, *sb = a.sb + (long long)kb * a.N + n0;
+        constexpr int waves = WM * WN;      // scales: 64 rows a load
+        const float *sa = a.sa + (long long)kb * a.M + m0, *sb = a.sb + kb * a.sb_ld + n0;
 #pragma unroll
         for (int i = 0; i < (BM / 64 + waves - 1) / waves; ++i) {
             const int part = i * waves + w;
@@ -205,8 +230,7 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int
         for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
     const int from_a = (wm * (BM / WM) + r) * 128 + ((g ^ (r & 7)) * 16);
     const int from_b = S::kA + (wn * 64 + 16 * (r >> 2) + (r & 3)) * 128 + ((g ^ (r & 7)) * 16);
-    const int nb = (a.N + 127) / 128;
-    const float *sb_at = a.sb + min((long long)(n0 + wn * 64) / 128, (long long)nb - 1);
+    const float *sb_at = a.sb + min((long long)(n0 + wn * 64) / 128, (a.N + 127LL) / 128 - 1);
     auto part = [&](const uint8_t *buf, int at) {
         Part<EXACT> p;
         p.set(*reinterpret_cast<const u32x4 *>(buf + at), *reinterpret_cast<const u32x4 *>(buf + (at ^ 64)));
@@ -216,7 +240,7 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int
     // block kb is in LDS for all wavefronts, and nobody reads the block before it any more
     auto arrive = [&](int kb) {
         __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): what this wavefront asked for is there
-        if (kb == nk - 1 && a.K % 128) {         // every thread clears behind K what it has brought itself
+        if (kb == blocks - 1 && a.K % 128) {     // every thread clears behind K what it has brought itself
             const int left = a.K - kb * 128;
 #pragma unroll
             for (int i = 0; i < (BM + BN) / kRound; ++i) {
@@ -229,11 +253,11 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int
     };
     // of squares, a wavefront's columns have one scale a block, read by the scalar unit: a vector load between the blocks on their way
     // to LDS would be waited for with them
-    auto square = [&](int kb) { return ROWS ? 0.f : ((const __attribute__((address_space(4))) float *)sb_at)[(long long)kb * nb]; };
-    float next = square(0);
-    fetch(0, buffer(0));
-    arrive(0);
-    if (nk > 1) fetch(1, buffer(1));
+    auto square = [&](int kb) { return ROWS ? 0.f : ((const __attribute__((address_space(4))) float *)sb_at)[kb * a.sb_ld]; };
+    float next = square(k0);
+    fetch(k0, buffer(k0));
+    arrive(k0);
+    if (k0 + 1 < nk) fetch(k0 + 1, buffer(k0 + 1));
     Part<EXACT> b[4], p[2];
     float scale[MT];      // of the rows of A
     auto scales = [&](const uint8_t *buf) {
@@ -242,9 +266,9 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int
         for (int i = 0; i < MT; ++i) scale[i] = sa[16 * i];
     };
 #pragma unroll
-    for (int j = 0; j < 4; ++j) b[j] = part(buffer(0), from_b + j * 512);
-    p[0] = part(buffer(0), from_a);
-    scales(buffer(0));
+    for (int j = 0; j < 4; ++j) b[j] = part(buffer(k0), from_b + j * 512);
+    p[0] = part(buffer(k0), from_a);
+    scales(buffer(k0));
     auto block = [&](int kb, auto final) {
         const uint8_t *buf = buffer(kb), *then = buffer(kb + 1);
         f32x4 sb[4];
@@ -295,57 +319,182 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int
             if (kb + 2 < nk) fetch(kb + 2, buffer(kb));
         }
     };
-    static_assert(MT % 2 == 0, "parts of A in turn");
-    for (int kb = 0; kb + 1 < nk; ++kb) block(kb, std::false_type{});
+    for (int kb = k0; kb + 1 < nk; ++kb) block(kb, std::false_type{});
     block(nk - 1, std::true_type{});
-    TO *C = static_cast<TO *>(a.C);
     const long long col = n0 + wn * 64 + 16 * g;
     const int left = (int)min(16LL, a.N - col);
-    const bool whole = left == 16 && (a.ldc * (long long)sizeof(TO)) % 16 == 0;
+    auto store = [&](auto *C, long long ldc) {
+        using To = std::remove_pointer_t<decltype(C)>;
+        const bool whole = left == 16 && (ldc * (long long)sizeof(To)) % 16 == 0;
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const long long m = m0 + wm * (BM / WM) + 16 * i + r;
-        if (m >= a.M) continue;
-        TO *to = C + m * a.ldc + col;
+        for (int i = 0; i < MT; ++i) {
+            const long long m = m0 + wm * (BM / WM) + 16 * i + r;
+            if (m >= a.M) continue;
+            To *to = C + m * ldc + col;
 #pragma unroll
-        for (int j = 0; j < 4; j += 2) {
-            const f32x8 v = __builtin_shufflevector(acc[i][j], acc[i][j + 1], 0, 1, 2, 3, 4, 5, 6, 7);
-            if (whole) store8<TO, true>(to + 4 * j, rounded<TO, true>(v), 8);
-            else store8<TO, false>(to + 4 * j, rounded<TO, false>(v), left - 4 * j);
+            for (int j = 0; j < 4; j += 2) {
+                const f32x8 v = __builtin_shufflevector(acc[i][j], acc[i][j + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+                if (whole) store8<To, true>(to + 4 * j, rounded<To, true>(v), 8);
+                else store8<To, false>(to + 4 * j, rounded<To, false>(v), left - 4 * j);
+            }
+        }
+    };
+    if (splits > 1) store(a.part + (long long)split * a.M * a.N, (long long)a.N);
+    else store(static_cast<TO *>(a.C), a.ldc);
+}
+
+// C = the sum of the splits' sums, in their order
+template <typename TO> __global__ __launch_bounds__(256) void matmul_join_kernel(Matmul a, int splits)
+{
+    const long long count = (long long)a.M * a.N;
+    TO *C = static_cast<TO *>(a.C);
+    for (long long i = ((long long)blockIdx.x * 256 + threadIdx.x) * 4; i < count; i += (long long)gridDim.x * 1024) {
+        const int here = (int)min(4LL, count - i);
+        f32x4 t = 0.f;
+        for (int s = 0; s < splits; ++s) {
+            const float *p = a.part + s * count + i;
+            if (count % 4 == 0) {
+                t += *reinterpret_cast<const f32x4 *>(p);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < here) t[e] += p[e];
+            }
+        }
+        long long m = i / a.N, n = i % a.N;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (e < here) put(C + m * a.ldc + n, t[e]);
+            if (++n == a.N) n = 0, ++m;
         }
     }
 }
 
+// How a product is shared out: the kernel for few rows (tile -1), or tiles and splits of K.
+constexpr int kTileRows[4] = {256, 128, 64, 128}, kTileCols[4] = {256, 128, 128, 64};      // (the first: 128 rows for fp32 results)
+// cols: columns of C that it takes; what is left is a product of its own, planned by itself.
+struct Plan { int tile, splits, cols; };
+
+// The cheapest by a model of each, in us, fitted to calls on an MI355X of 256 compute units (clocks differ by some per cent from
+// card to card; what it picked was within 11 % of the best of all for 22 sizes from 65 x 4096 x 4096 to 8192 x 64 x 4096):
+//   tiles      rounds of as many workgroups as a compute unit holds, each 1.5 us and so much a block of K, by how many
+//              share a compute unit; splits add the join: 4 us and their sums to memory and back
+//   few rows   B at 5 TB/s and the rows of A, read for every 16 rows of B, at 12 TB/s
+// Of tiles of 256 columns, a last column of tiles of which at most a quarter is there is left, where that is cheaper: the tiles of
+// 8192 x 20544 x 4096 are 10.1 rounds of workgroups, without the last 64 columns 10.
+Plan plan_of(int M, int N, int K, bool exact, double *cost = nullptr)
+{
+    // us a block of K of 1, 2, 3 workgroups a compute unit
+    static constexpr double kBlock[2][4][3] = {{{1.5}, {0.95, 1.28}, {0.72, 0.83, 1.15}, {0.72, 0.83, 1.15}},
+                                               {{1.75}, {1.55, 2.3}, {0.93, 1.35, 2.0}, {0.93, 1.35, 2.0}}};
+    static constexpr int kHeld[4] = {1, 2, 3, 3};
+    const int blocks = K / 128 + (K % 128 != 0), cus = device_cu_count();
+    Plan best = {0, 1, N};
+    double least = 1e30;
+    auto consider = [&](int t, int N, double besides) {
+        const int rows = t == 0 && exact ? 128 : kTileRows[t];
+        const double tiles = (double)((M + (long long)rows - 1) / rows) * (double)((N + (long long)kTileCols[t] - 1) / kTileCols[t]);
+        for (int s = 1; s <= 8 && (s == 1 || 2 * s <= blocks); s *= 2) {
+            const double groups = tiles * s, each = (double)((blocks + s - 1) / s), full = (double)((long long)(groups / (cus * kHeld[t])));
+            const int more = (int)((groups - full * cus * kHeld[t] + cus - 1) / cus);      // a compute unit in the last round
+            double us = 3 + full * (each * kBlock[exact][t][kHeld[t] - 1] + 1.5);
+            if (more > 0) us += each * kBlock[exact][t][more - 1] + 1.5;
+            if (s > 1) us += 4 + 2.0 * s * M * N * 4 / 4e6;
+            us += besides;
+            if (us < least) least = us, best = {t, s, N};
+        }
+    };
+    for (int t = 0; t < 4; ++t) consider(t, N, 0);
+    const int rest = N % kTileCols[0];
+    if (rest > 0 && rest <= kTileCols[0] / 4 && N > rest) {
+        double more = 0;
+        plan_of(M, rest, K, exact, &more);
+        consider(0, N - rest, more);
+    }
+    if (M <= 64) {
+        const double us = 3 + (double)N * K / 5e6 + (double)N / 16 * M * K / 12e6;
+        if (us < least || M <= 16) least = us, best = {-1, 1, N};
+    }
+    if (cost) *cost = least;
+    return best;
+}
+
 }  // namespace
 
-size_t matmul_workspace_bytes(int, int, int, int) { return 0; }
+size_t matmul_workspace_bytes(int M, int N, int K, int)
+{
+    size_t n = 0;
+    for (bool exact : {false, true}) {
+        for (int from = 0; from < N;) {
+            const Plan p = plan_of(M, N - from, K, exact);
+            if (p.splits > 1) n = std::max(n, (size_t)p.splits * M * p.cols * sizeof(float));
+            from += p.cols;
+        }
+    }
+    return n;
+}
 
-hipError_t launch_matmul(const Matmul &a, bool bf16_out, hipStream_t stream)
+hipError_t launch_matmul(const Matmul &whole, bool bf16_out, hipStream_t stream)
 {
     hipError_t status = hipSuccess;
-    auto launch = [&](auto one) {
-        auto rows = [&](auto MT) {
-            hipLaunchKernelGGL((matmul_rows_kernel<decltype(one), MT.value>),
-                               dim3((a.N + 15) / 16, (unsigned)((a.M + 16LL * MT.value - 1) / (16 * MT.value))), dim3(512), 0, stream, a);
-        };
-        if (a.M <= 16) return rows(std::integral_constant<int, 1>{});
-        if (a.M <= 64 || a.lda > (1 << 23) || a.ldb > (1 << 23)) return rows(std::integral_constant<int, 4>{});
-        auto tile = [&](auto by_rows) {
-            constexpr int BM = sizeof(one) == 4 ? 128 : 256, BN = 256, WM = 2, WN = 4;
-            using S = Tile<BM, BN, WM, WN, sizeof(one) == 4, by_rows.value>;
-            auto kernel = matmul_tile_kernel<decltype(one), BM, BN, WM, WN, by_rows.value>;
+    Matmul a = whole;
+    a.sb_ld = a.b_rows == 1 ? a.N : (a.N + 127LL) / 128;
+    auto launch = [&](auto one, const Plan &p) {
+        using TO = decltype(one);
+        constexpr bool EXACT = sizeof(TO) == 4;
+        if (p.tile < 0) {
+            auto rows = [&](auto MT, auto U) {
+                auto kernel = a.b_rows == 1 ? matmul_rows_kernel<TO, MT.value, U.value, true> : matmul_rows_kernel<TO, MT.value, U.value, false>;
+                hipLaunchKernelGGL(kernel, dim3((a.N + 15) / 16, (unsigned)((a.M + 16LL * MT.value - 1) / (16 * MT.value))), dim3(512), 0, stream, a);
+            };
+            using std::integral_constant;
+            if (a.M <= 16) rows(integral_constant<int, 1>{}, integral_constant<int, 4>{});
+            else if (a.M <= 32) rows(integral_constant<int, 2>{}, integral_constant<int, 2>{});
+            else rows(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+            return;
+        }
+        auto tile = [&](auto by_rows, auto bm, auto bn, auto wm, auto wn) {
+            constexpr int BM = bm.value, BN = bn.value, WM = wm.value, WN = wn.value;
+            using S = Tile<BM, BN, WM, WN, by_rows.value>;
+            auto kernel = matmul_tile_kernel<TO, BM, BN, WM, WN, by_rows.value>;
             static std::atomic<uint64_t> armed{0};
             const size_t bytes = 2 * S::kBuffer;
             status = arm_dynamic_lds(armed, reinterpret_cast<const void *>(kernel), bytes);
             if (status != hipSuccess) return;
             const int tm = (int)((a.M + (long long)BM - 1) / BM), tn = (int)((a.N + (long long)BN - 1) / BN);
-            hipLaunchKernelGGL(kernel, dim3((unsigned)tm * (unsigned)tn), dim3(S::kThreads), bytes, stream, a, tm, tn);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)tm * (unsigned)tn * p.splits), dim3(S::kThreads), bytes, stream, a, tm, tn, p.splits);
         };
-        if (a.b_rows == 1) tile(std::true_type{});
-        else tile(std::false_type{});
+        auto which = [&](auto by_rows) {
+            using std::integral_constant;
+            integral_constant<int, 1> c1;
+            integral_constant<int, 2> c2;
+            integral_constant<int, 4> c4;
+            integral_constant<int, 64> c64;
+            integral_constant<int, 128> c128;
+            integral_constant<int, 256> c256;
+            if (p.tile == 0) tile(by_rows, integral_constant<int, EXACT ? 128 : kTileRows[0]>{}, c256, c2, c4);
+            else if (p.tile == 1) tile(by_rows, c128, c128, c2, c2);
+            else if (p.tile == 2) tile(by_rows, c64, c128, c2, c2);
+            else tile(by_rows, c128, c64, c4, c1);
+        };
+        if (a.b_rows == 1) which(std::true_type{});
+        else which(std::false_type{});
+        if (p.splits > 1 && status == hipSuccess) {
+            const long long want = ((long long)a.M * a.N + 1023) / 1024, most = 8LL * device_cu_count();
+            hipLaunchKernelGGL(matmul_join_kernel<TO>, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, stream, a, p.splits);
+        }
     };
-    if (bf16_out) launch((bf16)0.f);
-    else launch(0.f);
+    for (int left = whole.N; left > 0 && status == hipSuccess;) {
+        Plan p = plan_of(a.M, left, a.K, !bf16_out);
+        if (a.lda > (1 << 23) || a.ldb > (1 << 23)) p = {-1, 1, left};      // (a tile's rows are reached by 32 bits)
+        a.N = p.cols;
+        if (bf16_out) launch((bf16)0.f, p);
+        else launch(0.f, p);
+        left -= p.cols;
+        a.B = static_cast<const uint8_t *>(a.B) + p.cols * a.ldb;
+        a.sb += a.b_rows == 1 ? p.cols : p.cols / 128;      // (what is left begins at a multiple of 256)
+        a.C = static_cast<uint8_t *>(a.C) + (size_t)p.cols * (bf16_out ? 2 : 4);
+    }
     return status == hipSuccess ? hipGetLastError() : status;
 }
 

@@ -249,10 +249,18 @@ def test_matmul(layer, M, N, K, b_rows):
     check_matmul(layer, M, N, K, b_rows, BF)
 
 
-@pytest.mark.parametrize("M,N,K", [(2048, 1024, 512), (1025, 2049, 1000), (2, 8192, 8192), (33, 4096, 4096)])
+@pytest.mark.parametrize("M,N,K", [(2048, 1024, 512), (1025, 2049, 1000), (2, 8192, 8192), (33, 4096, 4096), (300, 300, 8192), (130, 700, 8000)])
 def test_matmul_large(layer, M, N, K):
+    """Sizes of the large tiles, of few rows with many columns, and of K shared out between workgroups."""
     check_matmul(layer, M, N, K, 128, BF)
     check_matmul(layer, M, N, K, 1, F32)
+
+
+@pytest.mark.parametrize("b_rows", [1, 128])
+@pytest.mark.parametrize("N", [2112, 2050])
+def test_matmul_last_columns_apart(layer, N, b_rows):
+    """More tiles than compute units by a last column of them that is hardly there: a product of its own."""
+    check_matmul(layer, 8192, N, 1024, b_rows, BF)
 
 
 @pytest.mark.parametrize("M,N", [(5, 24), (300, 264), (300, 265)])
