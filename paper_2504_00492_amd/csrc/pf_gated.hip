@@ -74,7 +74,9 @@ template <typename T, int V, bool VEC> __device__ __forceinline__ Raw<T, V> fetc
     Raw<T, V> r = {};
     if constexpr (VEC) {
         if (left > 0) __builtin_memcpy(&r, __builtin_assume_aligned(p, sizeof(T) * V), sizeof(T) * V);
-    } else {
+    } else if (left >= V) {
+        __builtin_memcpy(&r, p, sizeof(T) * V);
+    } else if (left > 0) {
         T e[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) e[v] = v < left ? p[v] : (T)0.f;
@@ -94,6 +96,8 @@ template <typename T, int V, bool VEC> __device__ __forceinline__ void keep(T *p
     for (int v = 0; v < V; ++v) e[v] = (T)f[v];
     if constexpr (VEC) {
         if (left > 0) __builtin_memcpy(__builtin_assume_aligned(p, sizeof(T) * V), e, sizeof(e));
+    } else if (left >= V) {
+        __builtin_memcpy(p, e, sizeof(e));
     } else {
 #pragma unroll
         for (int v = 0; v < V; ++v)

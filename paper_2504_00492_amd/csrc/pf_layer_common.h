@@ -10,8 +10,8 @@ typedef float f32x8 __attribute__((ext_vector_type(8)));
 // whether rows from p on, `ld` elements of `size` bytes apart, begin at whole 16 bytes
 inline bool wide(const void *p, long long ld, int size) { return (reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size)) % 16 == 0; }
 
-// Eight consecutive values of a row of which `left` are there (more than 8: all; none: zeros).  VEC: the row and its place
-// allow 16-byte accesses and `left` is 0 or at least 8.
+// Eight consecutive values of a row of which `left` are there (more than 8: all; none: zeros).  VEC: their address is a multiple
+// of 16 and `left` is 0 or at least 8; else eight are still one access, which the hardware takes at any address.
 template <typename T, bool VEC> struct Raw8;      // as they lie in memory, on their way
 template <bool VEC> struct Raw8<bf16, VEC> { u32x4 v; };
 template <bool VEC> struct Raw8<float, VEC> { f32x4 v[2]; };
@@ -21,7 +21,9 @@ template <typename T, bool VEC> __device__ __forceinline__ Raw8<T, VEC> load8(co
     Raw8<T, VEC> r = {};
     if constexpr (VEC) {
         if (left > 0) __builtin_memcpy(&r, __builtin_assume_aligned(p, 16), sizeof(r));
-    } else {
+    } else if (left >= 8) {
+        __builtin_memcpy(&r, p, sizeof(r));
+    } else if (left > 0) {
         T e[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) e[i] = i < left ? p[i] : (T)0.f;
@@ -59,7 +61,9 @@ template <typename T, bool VEC> __device__ __forceinline__ void store8(T *p, con
 {
     if constexpr (VEC) {
         if (left > 0) __builtin_memcpy(__builtin_assume_aligned(p, 16), &r, sizeof(r));
-    } else {
+    } else if (left >= 8) {
+        __builtin_memcpy(p, &r, sizeof(r));
+    } else if (left > 0) {
         T e[8];
         __builtin_memcpy(e, &r, sizeof(r));
 #pragma unroll

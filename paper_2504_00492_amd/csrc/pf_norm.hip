@@ -176,18 +176,25 @@ __global__ __launch_bounds__(kThreads<G>) void norm_bwd_kernel(NormBwd a)
         store8<float, false>(a.part + (long long)blockIdx.x * a.D + col(i), rounded<float, false>(dw[i]), a.D - col(i));
 }
 
-// dw = sum of the workgroups' sums: 16 slices of them to a workgroup of 64 columns
+// dw = sum of the workgroups' sums: a workgroup takes 32 columns, 32 slices of the sums side by side, sixteen loads of a slice on
+// their way at once.
 __global__ __launch_bounds__(1024) void norm_dw_kernel(const float *part, float *dw, int parts, int D)
 {
-    __shared__ float s[16][64];
-    const int c = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6;
+    __shared__ float s[32][33];
+    const int x = threadIdx.x & 31, k = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
     float t = 0.f;
-    if (c < D)
-        for (int p = k; p < parts; p += 16) t += part[(long long)p * D + c];
-    s[k][threadIdx.x & 63] = t;
+    for (int p0 = k; p0 < parts; p0 += 32 * 16) {
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = c < D && p0 + 32 * i < parts ? part[(long long)(p0 + 32 * i) * D + c] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t += v[i];
+    }
+    s[k][x] = t;
     __syncthreads();
     if (k || c >= D) return;
-    for (int i = 1; i < 16; ++i) t += s[i][threadIdx.x & 63];
+#pragma unroll
+    for (int i = 1; i < 32; ++i) t += s[i][x];
     dw[c] = t;
 }
 
@@ -260,7 +267,7 @@ hipError_t launch_norm_bwd(const NormBwd &a, bool is_bf16, hipStream_t stream)
         if (is_bf16) by_type<bf16>(vec, launch);
         else by_type<float>(vec, launch);
     }
-    if (a.dw) hipLaunchKernelGGL(norm_dw_kernel, dim3((a.D + 63) / 64), dim3(1024), 0, stream, a.part, a.dw, parts, a.D);
+    if (a.dw) hipLaunchKernelGGL(norm_dw_kernel, dim3((a.D + 31) / 32), dim3(1024), 0, stream, a.part, a.dw, parts, a.D);
     return hipGetLastError();
 }
 
