@@ -98,7 +98,7 @@ pf_status pf_quant_fp8(const void *X, long long ldx, void *Q, long long ldq, flo
  *   sb  [ceil(K/128), N] (b_rows = 1) or [ceil(K/128), ceil(N/128)] (b_rows = 128)   fp32   in
  *   C   [M, N], row stride ldc     dt     out
  *   workspace / workspace_bytes           at least pf_matmul_fp8_workspace_bytes(...) bytes, overwritten (may be NULL
- *                                         when that is 0)
+ *                                         when that is 0, as for M up to 16)
  *
  * dt = PF_BF16: the sum over a block is the 8-bit matrix instruction's, which adds eight products at a time aligned to the
  * largest of them and drops what lies 2^-13 below that (1.4e-5 of the result's norm for normally distributed values).
@@ -129,7 +129,8 @@ pf_status pf_matmul_fp8(const void *A, long long lda, const float *sa, const voi
  *   Y   [B, L, D]                                   dt     out
  *   hL  [B, D]                                      fp32   out   NULL: not written.  hL == h0 is allowed
  *   workspace / workspace_bytes                     at least pf_gated_workspace_bytes(...) bytes, overwritten (may be
- *                                                   NULL when that is 0; the forward and the backward need the same)
+ *                                                   NULL when that is 0, as for L up to 16; the forward and the
+ *                                                   backward need the same)
  *
  * L == 0: hL receives h0 (or zeros), the sequence pointers may be NULL.  B == 0: nothing is done.
  * Where h overflows to infinity, later values may be NaN instead of infinite.

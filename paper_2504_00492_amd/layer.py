@@ -10,6 +10,8 @@ from __future__ import annotations
 import ctypes
 import os
 
+import torch
+
 from .binding import PF_BF16, PF_F32, PF_OK, PfError, _ptr, _stream_handle
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libpf_layer.so")
@@ -97,132 +99,175 @@ def pf_gated_bwd(X, xb, xt, G, gb, gt, h0, Y, dY, dyb, dyt, dhL, dX, dG, dh0, B,
 
 
 # ---- on torch tensors
+#
+# A small call is bound by what happens here (a launch alone takes the host 3.4 us), so every tensor is looked at in as few
+# steps as tell that it is right; _refuse finds out what is wrong with one that is not.
 
-def _dt(t, what):
-    import torch
-    if t.dtype == torch.bfloat16:
-        return PF_BF16
-    if t.dtype == torch.float32:
-        return PF_F32
-    raise ValueError(f"{what} must be float32 or bfloat16")
+_BF, _F32, _E4 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
+_DT = {_BF: PF_BF16, _F32: PF_F32}
+_empty, _like, _stream, _current = torch.empty, torch.empty_like, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
-def _check(t, what, shape, dtype, device, dense=True):
-    """t: None, or a tensor of this shape, type and device whose innermost dimension is contiguous (dense: all of it)."""
-    if t is None:
-        return
-    if t.device != device:
-        raise ValueError(f"{what} must be on {device}; there is no CPU path")
+def _refuse(t, what, shape, dtype, index):
+    if not t.is_cuda or t.get_device() != index:
+        raise ValueError(f"{what} must be on cuda:{index}; there is no CPU path")
     if t.dtype != dtype:
         raise ValueError(f"{what} must be {dtype}")
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{what} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
-    if dense and not t.is_contiguous():
-        raise ValueError(f"{what} must be contiguous")
-    if not dense and t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+    raise ValueError(f"{what} must be contiguous")
+
+
+def _first(t, what, dims):
+    """Type code and device index of the tensor that the others go by."""
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a CUDA (HIP) tensor; there is no CPU path")
+    if t.dim() != dims:
+        raise ValueError(f"{what} must have {('two', 'three')[dims - 2]} dimensions")
+    dt = _DT.get(t.dtype)
+    if dt is None:
+        raise ValueError(f"{what} must be float32 or bfloat16")
+    return dt, t.get_device()
+
+
+def _dense(t, what, shape, dtype, index):
+    """Address of a contiguous tensor of this shape and type, or None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or not t.is_contiguous():
+        _refuse(t, what, shape, dtype, index)
+    return t.data_ptr()
+
+
+def _inner(t, what):
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"the innermost dimension of {what} must be contiguous")
 
 
-def _gpu(t, what):
-    if not t.is_cuda:
-        raise ValueError(f"{what} must be a CUDA (HIP) tensor; there is no CPU path")
-    return t.device
+def _rows(t, what, shape, dtype, index):
+    """Address and row stride of a matrix whose rows may lie apart (any stride serves where there is but one row)."""
+    if t is None:
+        return None, 0
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
+        _refuse(t, what, shape, dtype, index)
+    if t.is_contiguous():
+        return t.data_ptr(), shape[1]
+    _inner(t, what)
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else max(shape[1], t.stride(0))
 
 
-def _row(t):
-    """Row stride of a matrix (any value serves where there is but one row)."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+def _steps(t, what, shape, dtype, index):
+    """Address, batch and token stride of [B, L, D] (where there is but one of them, what a dense array would have)."""
+    if t is None:
+        return None, 0, 0
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
+        _refuse(t, what, shape, dtype, index)
+    B, L, D = shape
+    if t.is_contiguous():
+        return t.data_ptr(), L * D, D
+    _inner(t, what)
+    token = t.stride(1) if L > 1 else D
+    return t.data_ptr(), t.stride(0) if B > 1 else L * token, token
 
 
 def _byte_rows(M, K, device):
     """An uninitialised e4m3 matrix whose rows lie a multiple of 16 bytes apart."""
-    import torch
-    ld = (K + 15) // 16 * 16
-    q = torch.empty((M, ld), dtype=torch.float8_e4m3fn, device=device)
+    ld = -(-K // 16) * 16
+    q = _empty((M, ld), dtype=_E4, device=device)
     return q if ld == K else q[:, :K]
 
 
-def _byte_row(t, what):
-    """Row stride of an e4m3 matrix, whose last row too must be held in whole 16 bytes."""
-    rows, whole = t.shape[0], (t.shape[1] + 15) // 16 * 16
+def _byte_matrix(t, what, shape, index):
+    """Address and row stride of an e4m3 matrix, whose last row too must be held in whole 16 bytes."""
+    if t.dtype is not _E4 or t.get_device() != index or t.shape != shape:
+        _refuse(t, what, shape, _E4, index)
+    rows, K = shape
+    if K % 16 == 0 and t.is_contiguous():
+        return t.data_ptr(), K
+    _inner(t, what)
+    whole = -(-K // 16) * 16
     ld = t.stride(0) if rows > 1 else max(whole, t.stride(0) // 16 * 16)
     if rows and t.storage_offset() + (rows - 1) * ld + whole > t.untyped_storage().nbytes():
         raise ValueError(f"the rows of {what} must be held in a multiple of 16 bytes")
-    return ld
+    return t.data_ptr(), ld
 
 
-def _stream_of(device, stream):
-    import torch
-    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else _stream_handle(stream)
-
-
-def _call(fn, name, device, args):
-    """One library call with `device` as the current one."""
-    import torch
-    if torch._C._cuda_getDevice() == device.index:
-        st = fn(*args)
-    else:
-        with torch.cuda.device(device):
-            st = fn(*args)
-    if st != PF_OK:
-        raise PfError(st, name)
+def _same(t):
+    """An uninitialised dense tensor of t's shape and type (0.5 us less than naming both, where t is dense itself)."""
+    return _like(t) if t.is_contiguous() else _empty(t.shape, dtype=t.dtype, device=t.device)
 
 
 def _workspace(need, given, device):
-    """(address, bytes) of the workspace handed in, or of a new one; the tensor is kept until the call has been made."""
-    import torch
+    """(tensor, address, bytes) of the workspace handed in, or of a new one; the tensor is kept until the call has been made."""
     if given is None:
         if not need:
             return None, None, 0
-        given = torch.empty(need, dtype=torch.uint8, device=device)
+        given = _empty(need, dtype=torch.uint8, device=device)
     return given, given.data_ptr(), given.numel() * given.element_size()
+
+
+def _call(fn, name, index, stream, *args):
+    """One library call with the tensors' device as the current one, on its current stream unless one is given."""
+    stream = _stream(index) if stream is None else _stream_handle(stream)
+    if _current() == index:
+        st = fn(*args, stream)
+    else:
+        with torch.cuda.device(index):
+            st = fn(*args, stream)
+    if st != PF_OK:
+        raise PfError(st, name)
 
 
 def norm_fwd(X, w=None, R=None, *, eps, y: bool = True, fp8: bool = False, inplace: bool = False, stream=None):
     """Root-mean-square norm of the rows of X + R (pf_norm_fwd).  X, R [M, D] (float32 or bfloat16, rows may lie apart), w [D]
     of the same type.  Returns (S, Y, Q, scale): S the stored sum (X itself without R; R's own memory with inplace, which
     asks for a contiguous R), Y the norm (None with y=False), Q and scale the norm in 8 bits (None unless fp8)."""
-    import torch
-    device, dt = _gpu(X, "X"), _dt(X, "X")
-    if X.dim() != 2:
-        raise ValueError("X must have two dimensions")
-    M, D = X.shape
-    _check(X, "X", (M, D), X.dtype, device, dense=False)
-    _check(R, "R", (M, D), X.dtype, device, dense=inplace)
-    _check(w, "w", (D,), X.dtype, device)
+    dt, index = _first(X, "X", 2)
+    shape, dtype = X.shape, X.dtype
+    M, D = shape
+    xp, ldx = _rows(X, "X", shape, dtype, index)
+    rp, ldr = _rows(R, "R", shape, dtype, index)
+    wp = _dense(w, "w", (D,), dtype, index)
     if not (y or fp8):
         raise ValueError("neither y nor fp8 is wanted")
-    if inplace and R is None:
-        raise ValueError("inplace needs R")
-    S = X if R is None else R if inplace else torch.empty((M, D), dtype=X.dtype, device=device)
-    Y = torch.empty((M, D), dtype=X.dtype, device=device) if y else None
-    Q = scale = None
+    if inplace:
+        if R is None:
+            raise ValueError("inplace needs R")
+        _dense(R, "R", shape, dtype, index)
+    device = X.device
+    S, sp = X, None
+    if R is not None:
+        S = R if inplace else _same(X)
+        sp = S.data_ptr()
+    Y = yp = Q = qp = scale = cp = None
+    if y:
+        Y = _same(X)
+        yp = Y.data_ptr()
     if fp8:
-        Q, scale = _byte_rows(M, D, device), torch.empty((-(-D // 128), M), dtype=torch.float32, device=device)
-    _call(_lib.pf_norm_fwd, "pf_norm_fwd", device, (
-        X.data_ptr(), _row(X), _ptr(R), 0 if R is None else _row(R), _ptr(w), None if R is None else S.data_ptr(), _ptr(Y), _ptr(Q),
-        (D + 15) // 16 * 16, _ptr(scale), M, D, eps, dt, _stream_of(device, stream)))
+        Q, scale = _byte_rows(M, D, device), _empty((-(-D // 128), M), dtype=_F32, device=device)
+        qp, cp = Q.data_ptr(), scale.data_ptr()
+    _call(_lib.pf_norm_fwd, "pf_norm_fwd", index, stream, xp, ldx, rp, ldr, wp, sp, yp, qp, -(-D // 16) * 16, cp, M, D, eps, dt)
     return S, Y, Q, scale
 
 
 def norm_bwd(S, dY, w=None, dS=None, *, eps, want_dw: bool = True, workspace=None, stream=None):
     """Backward of norm_fwd (pf_norm_bwd): S the stored sum, dY the gradient of the norm, dS that of the sum past the norm
     (None: none).  Returns (dX, dw): dX [M, D] in the inputs' type, dw [D] in float32 (None unless wanted)."""
-    import torch
-    device, dt = _gpu(S, "S"), _dt(S, "S")
-    if S.dim() != 2:
-        raise ValueError("S must have two dimensions")
-    M, D = S.shape
-    _check(S, "S", (M, D), S.dtype, device, dense=False)
-    _check(dY, "dY", (M, D), S.dtype, device, dense=False)
-    _check(dS, "dS", (M, D), S.dtype, device, dense=False)
-    _check(w, "w", (D,), S.dtype, device)
-    dX = torch.empty((M, D), dtype=S.dtype, device=device)
-    dw = torch.empty(D, dtype=torch.float32, device=device) if want_dw else None
-    keep, wp, wb = _workspace(_lib.pf_norm_bwd_workspace_bytes(M, D) if want_dw else 0, workspace, device)
-    _call(_lib.pf_norm_bwd, "pf_norm_bwd", device, (
-        S.data_ptr(), _row(S), _ptr(w), dY.data_ptr(), _row(dY), _ptr(dS), 0 if dS is None else _row(dS), dX.data_ptr(), _ptr(dw),
-        M, D, eps, dt, wp, wb, _stream_of(device, stream)))
+    dt, index = _first(S, "S", 2)
+    shape, dtype, device = S.shape, S.dtype, S.device
+    M, D = shape
+    sp, lds = _rows(S, "S", shape, dtype, index)
+    yp, ldy = _rows(dY, "dY", shape, dtype, index)
+    rp, ldr = _rows(dS, "dS", shape, dtype, index)
+    wp = _dense(w, "w", (D,), dtype, index)
+    dX = _same(S)
+    dw = dp = keep = kp = None
+    kb = 0
+    if want_dw:
+        dw = _empty(D, dtype=_F32, device=device)
+        dp = dw.data_ptr()
+        keep, kp, kb = _workspace(_lib.pf_norm_bwd_workspace_bytes(M, D) if workspace is None else 0, workspace, device)
+    _call(_lib.pf_norm_bwd, "pf_norm_bwd", index, stream, sp, lds, wp, yp, ldy, rp, ldr, dX.data_ptr(), dp, M, D, eps, dt, kp, kb)
     return dX, dw
 
 
@@ -230,51 +275,52 @@ def quant_fp8(X, *, rows: int = 1, plain: bool = True, transposed: bool = False,
     """X [M, K] (float32 or bfloat16, rows may lie apart) in 8 bits (pf_quant_fp8), with a scale for each row and 128 columns
     (rows=1) or each 128 x 128 (rows=128).  Returns (Q, scale, QT, scaleT); Q and scale are None with plain=False, QT and
     scaleT (the transposed matrix, its blocks along its own rows) unless transposed."""
-    import torch
-    device, dt = _gpu(X, "X"), _dt(X, "X")
-    if X.dim() != 2:
-        raise ValueError("X must have two dimensions")
+    dt, index = _first(X, "X", 2)
     M, K = X.shape
-    _check(X, "X", (M, K), X.dtype, device, dense=False)
+    xp, ldx = _rows(X, "X", X.shape, X.dtype, index)
     if rows not in (1, 128):
         raise ValueError("rows must be 1 or 128")
     if not (plain or transposed):
         raise ValueError("neither plain nor transposed is wanted")
-    Q = scale = QT = scaleT = None
-    per = lambda n: n if rows == 1 else -(-n // 128)      # noqa: E731
+    device = X.device
+    Q = qp = scale = sp = QT = tp = scaleT = up = None
     if plain:
-        Q, scale = _byte_rows(M, K, device), torch.empty((-(-K // 128), per(M)), dtype=torch.float32, device=device)
+        Q = _byte_rows(M, K, device)
+        scale = _empty((-(-K // 128), M if rows == 1 else -(-M // 128)), dtype=_F32, device=device)
+        qp, sp = Q.data_ptr(), scale.data_ptr()
     if transposed:
-        QT, scaleT = _byte_rows(K, M, device), torch.empty((-(-M // 128), per(K)), dtype=torch.float32, device=device)
-    _call(_lib.pf_quant_fp8, "pf_quant_fp8", device, (
-        X.data_ptr(), _row(X), _ptr(Q), (K + 15) // 16 * 16, _ptr(scale), _ptr(QT), (M + 15) // 16 * 16, _ptr(scaleT), M, K, rows,
-        dt, _stream_of(device, stream)))
+        QT = _byte_rows(K, M, device)
+        scaleT = _empty((-(-M // 128), K if rows == 1 else -(-K // 128)), dtype=_F32, device=device)
+        tp, up = QT.data_ptr(), scaleT.data_ptr()
+    _call(_lib.pf_quant_fp8, "pf_quant_fp8", index, stream, xp, ldx, qp, -(-K // 16) * 16, sp, tp, -(-M // 16) * 16, up, M, K, rows, dt)
     return Q, scale, QT, scaleT
 
 
-def matmul_fp8(A, sa, B, sb, *, b_rows: int = 128, out_dtype=None, workspace=None, stream=None):
+def matmul_fp8(A, sa, B, sb, *, b_rows: int = 128, out_dtype=_BF, workspace=None, stream=None):
     """C [M, N] = A [M, K] times B [N, K] transposed, both e4m3 with scales (pf_matmul_fp8): sa [ceil(K/128), M], sb
     [ceil(K/128), N] (b_rows=1) or [ceil(K/128), ceil(N/128)] (b_rows=128).  Rows of A and B lie a multiple of 16 bytes apart,
-    as quant_fp8 and norm_fwd lay them.  out_dtype: bfloat16 (the default) or float32."""
-    import torch
-    device = _gpu(A, "A")
+    as quant_fp8 and norm_fwd lay them.  out_dtype: bfloat16 or float32."""
+    if not A.is_cuda:
+        raise ValueError("A must be a CUDA (HIP) tensor; there is no CPU path")
     if A.dim() != 2 or B.dim() != 2:
         raise ValueError("A and B must have two dimensions")
     if b_rows not in (1, 128):
         raise ValueError("b_rows must be 1 or 128")
-    out_dtype = torch.bfloat16 if out_dtype is None else out_dtype
-    (M, K), N = A.shape, B.shape[0]
+    dt = _DT.get(out_dtype)
+    if dt is None:
+        raise ValueError("out_dtype must be float32 or bfloat16")
+    index, device = A.get_device(), A.device
+    M, K = A.shape
+    N = B.shape[0]
     nk = -(-K // 128)
-    _check(A, "A", (M, K), torch.float8_e4m3fn, device, dense=False)
-    _check(B, "B", (N, K), torch.float8_e4m3fn, device, dense=False)
-    _check(sa, "sa", (nk, M), torch.float32, device)
-    _check(sb, "sb", (nk, N if b_rows == 1 else -(-N // 128)), torch.float32, device)
-    C = torch.empty((M, N), dtype=out_dtype, device=device)
-    dt = _dt(C, "out_dtype")
-    keep, wp, wb = _workspace(_lib.pf_matmul_fp8_workspace_bytes(M, N, K, b_rows), workspace, device)
-    _call(_lib.pf_matmul_fp8, "pf_matmul_fp8", device, (
-        A.data_ptr(), _byte_row(A, "A"), sa.data_ptr(), B.data_ptr(), _byte_row(B, "B"), sb.data_ptr(), b_rows, C.data_ptr(), N, M, N,
-        K, dt, wp, wb, _stream_of(device, stream)))
+    ap, lda = _byte_matrix(A, "A", (M, K), index)
+    bp, ldb = _byte_matrix(B, "B", (N, K), index)
+    sap = _dense(sa, "sa", (nk, M), _F32, index)
+    sbp = _dense(sb, "sb", (nk, N if b_rows == 1 else -(-N // 128)), _F32, index)
+    C = _empty((M, N), dtype=out_dtype, device=device)
+    # (16 rows at most never need a workspace)
+    keep, kp, kb = _workspace(_lib.pf_matmul_fp8_workspace_bytes(M, N, K, b_rows) if workspace is None and M > 16 else 0, workspace, device)
+    _call(_lib.pf_matmul_fp8, "pf_matmul_fp8", index, stream, ap, lda, sap, bp, ldb, sbp, b_rows, C.data_ptr(), N, M, N, K, dt, kp, kb)
     return C
 
 
@@ -284,54 +330,41 @@ def _gate_of(gate):
     return GATES[gate]
 
 
-def _steps(t):
-    """Batch and token strides of [B, L, D] (where there is but one of them, what a dense array would have)."""
-    B, L, D = t.shape
-    token = t.stride(1) if L > 1 else D
-    return (t.stride(0) if B > 1 else L * token), token
-
-
 def gated_fwd(X, G, h0=None, *, gate: str = "log", mix: bool = False, workspace=None, stream=None):
     """The gated linear recurrence h_t = a_t h_{t-1} + b_t (pf_gated_fwd): a = G, exp(G) or its sigmoid by gate ("value",
     "log", "logit"), b = X, or (1 - a) X with mix.  X, G [B, L, D] (float32 or bfloat16, tokens and sequences may lie apart or in the
     other order), h0 [B, D] float32 or None.  Returns (Y [B, L, D], h_L [B, D] float32)."""
-    import torch
-    device, dt, form = _gpu(X, "X"), _dt(X, "X"), _gate_of(gate)
-    if X.dim() != 3:
-        raise ValueError("X must have three dimensions")
-    B, L, D = X.shape
-    _check(X, "X", (B, L, D), X.dtype, device, dense=False)
-    _check(G, "G", (B, L, D), X.dtype, device, dense=False)
-    _check(h0, "h0", (B, D), torch.float32, device)
-    Y = torch.empty((B, L, D), dtype=X.dtype, device=device)
-    hL = torch.empty((B, D), dtype=torch.float32, device=device)
-    keep, wp, wb = _workspace(_lib.pf_gated_workspace_bytes(B, L, D, dt), workspace, device)
-    _call(_lib.pf_gated_fwd, "pf_gated_fwd", device, (
-        X.data_ptr(), *_steps(X), G.data_ptr(), *_steps(G), _ptr(h0), Y.data_ptr(), hL.data_ptr(), B, L, D, form, int(mix), dt, wp, wb,
-        _stream_of(device, stream)))
+    dt, index = _first(X, "X", 3)
+    form = _gate_of(gate)
+    shape, dtype, device = X.shape, X.dtype, X.device
+    B, L, D = shape
+    x = _steps(X, "X", shape, dtype, index)
+    g = _steps(G, "G", shape, dtype, index)
+    hp = _dense(h0, "h0", (B, D), _F32, index)
+    Y, hL = _same(X), _empty((B, D), dtype=_F32, device=device) if h0 is None else _like(h0)
+    # (16 tokens at most never need a workspace)
+    keep, kp, kb = _workspace(_lib.pf_gated_workspace_bytes(B, L, D, dt) if workspace is None and L > 16 else 0, workspace, device)
+    _call(_lib.pf_gated_fwd, "pf_gated_fwd", index, stream, *x, *g, hp, Y.data_ptr(), hL.data_ptr(), B, L, D, form, bool(mix), dt, kp, kb)
     return Y, hL
 
 
 def gated_bwd(X, G, Y, dY, h0=None, dhL=None, *, gate: str = "log", mix: bool = False, workspace=None, stream=None):
     """Backward of gated_fwd (pf_gated_bwd) from what it was given and returned (X may be None without mix), dY the gradient of
     Y, dhL that of h_L (float32, None: none).  Returns (dX, dG, dh0)."""
-    import torch
-    device, dt, form = _gpu(G, "G"), _dt(G, "G"), _gate_of(gate)
-    if G.dim() != 3:
-        raise ValueError("G must have three dimensions")
+    dt, index = _first(G, "G", 3)
+    form = _gate_of(gate)
     if mix and X is None:
         raise ValueError("mix needs X")
-    B, L, D = G.shape
-    _check(X, "X", (B, L, D), G.dtype, device, dense=False)
-    _check(G, "G", (B, L, D), G.dtype, device, dense=False)
-    _check(Y, "Y", (B, L, D), G.dtype, device)
-    _check(dY, "dY", (B, L, D), G.dtype, device, dense=False)
-    _check(h0, "h0", (B, D), torch.float32, device)
-    _check(dhL, "dhL", (B, D), torch.float32, device)
-    dX, dG = (torch.empty((B, L, D), dtype=G.dtype, device=device) for _ in range(2))
-    dh0 = torch.empty((B, D), dtype=torch.float32, device=device)
-    keep, wp, wb = _workspace(_lib.pf_gated_workspace_bytes(B, L, D, dt), workspace, device)
-    _call(_lib.pf_gated_bwd, "pf_gated_bwd", device, (
-        _ptr(X), *((0, 0) if X is None else _steps(X)), G.data_ptr(), *_steps(G), _ptr(h0), Y.data_ptr(), dY.data_ptr(), *_steps(dY),
-        _ptr(dhL), dX.data_ptr(), dG.data_ptr(), dh0.data_ptr(), B, L, D, form, int(mix), dt, wp, wb, _stream_of(device, stream)))
+    shape, dtype, device = G.shape, G.dtype, G.device
+    B, L, D = shape
+    x = _steps(X, "X", shape, dtype, index)
+    g = _steps(G, "G", shape, dtype, index)
+    yp = _dense(Y, "Y", shape, dtype, index)
+    dy = _steps(dY, "dY", shape, dtype, index)
+    hp, ep = _dense(h0, "h0", (B, D), _F32, index), _dense(dhL, "dhL", (B, D), _F32, index)
+    dX, dG = _same(G), _same(G)
+    dh0 = _empty((B, D), dtype=_F32, device=device) if h0 is None else _like(h0)
+    keep, kp, kb = _workspace(_lib.pf_gated_workspace_bytes(B, L, D, dt) if workspace is None and L > 16 else 0, workspace, device)
+    _call(_lib.pf_gated_bwd, "pf_gated_bwd", index, stream, *x, *g, hp, yp, *dy, ep, dX.data_ptr(), dG.data_ptr(), dh0.data_ptr(), B, L, D,
+          form, bool(mix), dt, kp, kb)
     return dX, dG, dh0

@@ -134,6 +134,13 @@ def test_nothing_to_do(layer):
     assert layer.pf_matmul_fp8_workspace_bytes(0, 1, 1, 1) == 0
 
 
+def test_small_calls_need_no_workspace(layer):
+    for n in (1, 2, 15, 16):
+        for wide in (1, 100, 4096, 20544):
+            assert layer.pf_matmul_fp8_workspace_bytes(n, wide, 8192, 1) == layer.pf_matmul_fp8_workspace_bytes(n, wide, 8192, 128) == 0
+            assert layer.pf_gated_workspace_bytes(7, n, wide, BF16) == layer.pf_gated_workspace_bytes(7, n, wide, F32) == 0
+
+
 def test_workspace_is_bounded(layer):
     for M in (1, 7, 4096, 10**6):
         for D in (1, 128, 4096, 16384):
