@@ -204,25 +204,31 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int
     const int row = threadIdx.x >> 3, place = threadIdx.x & 7;
     const int piece_a = (place ^ (row & 7)) * 16, piece_b = (place ^ ((row & 3) | (row >> 2 & 4))) * 16;
     const uint32_t at_a = row * lda + piece_a, at_b = row * ldb + piece_b;
-    auto fetch = [&](int kb, uint8_t *buf) {      // (behind a row's end: the next row's values, taken out below)
-#pragma unroll
-        for (int i = 0; i < BM / kRound; ++i) to_lds16(A, at_a + (kb * 128 + i * kRound * lda), buf + (i * kRound * 128 + w * 1024));
-#pragma unroll
-        for (int i = 0; i < BN / kRound; ++i) to_lds16(B, at_b + (kb * 128 + i * kRound * ldb), buf + S::kA + (i * kRound * 128 + w * 1024));
-        constexpr int waves = WM * WN;      // scales: 64 rows a load
+    // Loads lo .. hi - 1 of the kLoads that bring block kb to LDS: rows of A, rows of B, scales (64 rows a load).  Behind a
+    // row's end come the next row's values, taken out below.
+    constexpr int waves = WM * WN, loads_a = BM / kRound, loads_b = BN / kRound, scales_a = (BM / 64 + waves - 1) / waves;
+    constexpr int kLoads = loads_a + loads_b + scales_a + (ROWS ? (BN / 64 + waves - 1) / waves : 0);
+    auto fetch = [&](int kb, uint8_t *buf, auto lo, auto hi) {
         const float *sa = a.sa + (long long)kb * a.M + m0, *sb = a.sb + kb * a.sb_ld + n0;
 #pragma unroll
-        for (int i = 0; i < (BM / 64 + waves - 1) / waves; ++i) {
-            const int part = i * waves + w;
-            if (part < BM / 64) to_lds4(sa + min(part * 64 + lane, rows_a - 1), buf + S::kA + S::kB + part * 256);
-        }
-        if constexpr (ROWS)
-#pragma unroll
-            for (int i = 0; i < (BN / 64 + waves - 1) / waves; ++i) {
-                const int part = i * waves + (waves - 1 - w);
+        for (int l = lo.value; l < (hi.value < kLoads ? hi.value : kLoads); ++l) {
+            if (l < loads_a) {
+                to_lds16(A, at_a + (kb * 128 + l * kRound * lda), buf + (l * kRound * 128 + w * 1024));
+            } else if (l < loads_a + loads_b) {
+                const int i = l - loads_a;
+                to_lds16(B, at_b + (kb * 128 + i * kRound * ldb), buf + S::kA + (i * kRound * 128 + w * 1024));
+            } else if (l < loads_a + loads_b + scales_a) {
+                const int part = (l - loads_a - loads_b) * waves + w;
+                if (part < BM / 64) to_lds4(sa + min(part * 64 + lane, rows_a - 1), buf + S::kA + S::kB + part * 256);
+            } else {
+                const int part = (l - loads_a - loads_b - scales_a) * waves + (waves - 1 - w);
                 if (part < BN / 64) to_lds4(sb + min(part * 64 + lane, rows_b - 1), buf + S::kA + S::kB + 4 * BM + part * 256);
             }
+        }
     };
+    using std::integral_constant;
+    constexpr integral_constant<int, 0> none{};
+    constexpr integral_constant<int, kLoads> all{};
     f32x4 acc[MT][4];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
@@ -255,9 +261,14 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int
     // to LDS would be waited for with them
     auto square = [&](int kb) { return ROWS ? 0.f : ((const __attribute__((address_space(4))) float *)sb_at)[kb * a.sb_ld]; };
     float next = square(k0);
-    fetch(k0, buffer(k0));
+    // Loads of the block after the next that are asked for at once, the others at the next block's beginning: a few at a time, since
+    // they take a wavefront longer to ask for than a product takes (8192 x 8192 x 8192 472 -> 450 us); but all where a block is
+    // short (1024 x 4096 x 4096 29.0 -> 27.4)
+    constexpr int kEarly = MT > 2 ? 4 : kLoads;
+    constexpr integral_constant<int, kEarly> early{};
+    fetch(k0, buffer(k0), none, all);
     arrive(k0);
-    if (k0 + 1 < nk) fetch(k0 + 1, buffer(k0 + 1));
+    if (k0 + 1 < nk) fetch(k0 + 1, buffer(k0 + 1), none, early);
     Part<EXACT> b[4], p[2];
     float scale[MT];      // of the rows of A
     auto scales = [&](const uint8_t *buf) {
@@ -299,6 +310,13 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int
 #pragma unroll
             for (int j = 0; j < 2; ++j) c[h % 2][j] = product(b[h % 2 * 2 + j], p[i % 2]);
             if (h > 0) add(h - 1);
+            if constexpr (!final.value) {
+                if (h == 0) fetch(kb + 1, buffer(kb + 1), early, integral_constant<int, kEarly + 2>{});
+                if (h == 1) fetch(kb + 1, buffer(kb + 1), integral_constant<int, kEarly + 2>{}, integral_constant<int, kEarly + 4>{});
+                if (h == 2) fetch(kb + 1, buffer(kb + 1), integral_constant<int, kEarly + 4>{}, all);
+                if (h == 2 * MT - 2 && kb + 2 < nk) fetch(kb + 2, buffer(kb), none, integral_constant<int, kEarly / 2>{});
+                if (h == 2 * MT - 1 && kb + 2 < nk) fetch(kb + 2, buffer(kb), integral_constant<int, kEarly / 2>{}, early);
+            }
             if (!final.value && h >= 2 * MT - 2)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) b[h % 2 * 2 + j] = part(then, from_b + (h % 2 * 2 + j) * 512);
@@ -314,10 +332,7 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int
             if (!final.value && h == 2 * MT - 3) arrive(kb + 1);
         }
         add(2 * MT - 1);
-        if constexpr (!final.value) {
-            scales(then);
-            if (kb + 2 < nk) fetch(kb + 2, buffer(kb));
-        }
+        if constexpr (!final.value) scales(then);
     };
     for (int kb = k0; kb + 1 < nk; ++kb) block(kb, std::false_type{});
     block(nk - 1, std::true_type{});
