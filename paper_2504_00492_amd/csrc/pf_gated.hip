@@ -25,10 +25,10 @@ namespace pf {
 namespace {
 
 constexpr int kWaves = 8, kWalkSteps = 16;
-// Steps of a wavefront's span of a tile: as many as the registers hold two workgroups to a compute unit of (forward two
-// arrays, backward four); longer tiles have fewer words to tell and to wait for (1 x 65536 x 4096, bf16: 16 steps 351 us,
-// 24 320).
-template <typename T, bool BACK> constexpr int kTileSteps = BACK ? 16 : sizeof(T) == 2 ? 24 : 32;
+// Steps of a wavefront's span of a tile, as its registers allow: forward (two arrays) two workgroups to a compute unit, of tiles that are
+// long, so that there is less to tell and to wait for (1 x 65536 x 4096, bf16: 16 steps 351 us, 24 320); backward (up to four
+// arrays) three of short ones (2 x 8192 x 4096: two of 16 steps 188 us, three of 9 183; 16 x 2048 x 4096 316 and 314).
+template <typename T, bool BACK> constexpr int kTileSteps = BACK ? 9 : sizeof(T) == 2 ? 24 : 32;
 template <typename T> inline int tile_tokens(bool back) { return kWaves * (back ? kTileSteps<T, true> : kTileSteps<T, false>); }
 
 // the decay a, 1 - a, and d a / d g of a gate's value
@@ -464,10 +464,9 @@ __global__ __launch_bounds__(64 * kWaves) void gated_walk_kernel(Gated a, int gr
     __shared__ Pair spans[2][kWaves][V][64];
     by_form<T, V, VEC, BACK, MIX>(a.gate, [&](auto k) { gated_walk<decltype(k)>(a, groups, spans); });
 }
-// (four wavefronts to a SIMD: two workgroups to a compute unit, so that one reads while the other waits; where channels lie at
-// odd places their registers allow three)
+// (so many wavefronts to a SIMD; where channels lie at odd places their registers allow three)
 template <typename T, int V, bool VEC, bool BACK, bool MIX>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(VEC ? 4 : 3)))
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(!VEC ? 3 : BACK ? 6 : 4)))
 void gated_tile_kernel(Gated a, int groups, int chains, int tiles, Work work)
 {
     __shared__ TileLds<V> lds;

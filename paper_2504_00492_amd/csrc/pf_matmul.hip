@@ -159,7 +159,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(4))) void m
 // sixteen lanes that read the same piece of sixteen rows meet different banks: the key is what tells apart eight neighbouring
 // lanes of a read, the row's last three bits for A, and for B, whose lanes go over rows 16 (r >> 2) + (r & 3) so that a lane ends up with
 // 16 neighbouring columns of C, two bits from either part.
-template <int BM, int BN, int WM, int WN, bool ROWS> struct Tile {
+template <int BM, int BN, int WM, int WN, int KG, bool ROWS> struct Tile {
     static constexpr int kThreads = 64 * WM * WN, MT = BM / WM / 16;
     static_assert(BN / WN == 64 && kThreads >= 256 && MT % 2 == 0, "a wavefront has 64 columns, a load 32 rows, parts of A take turns");
     static constexpr int kA = BM * 128, kB = BN * 128, kBuffer = kA + kB + 4 * BM + (ROWS ? 4 * BN : 0);
@@ -179,15 +179,20 @@ __device__ __forceinline__ void to_lds4(const void *g, void *l)
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)g, (__attribute__((address_space(3))) void *)l, 4, 0, 0);
 }
 
+// KG > 1: so many groups of WM x WN wavefronts share K between them, each with blocks in LDS of its own, and join at the end: where
+// tiles are few, one group is bound by how long a block takes from its arrival to its last sum, not by what it does (512 x 4096 x
+// 4096, 256 tiles: 23.6 us with one group, 27.6 with K split between workgroups, 17.9 with two groups).
 // splits > 1: each of so many workgroups of a tile takes a part of K and leaves its sums in a.part, [split][M][N].
-template <typename TO, int BM, int BN, int WM, int WN, bool ROWS>
-__global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int tiles_m, int tiles_n, int splits)
+template <typename TO, int BM, int BN, int WM, int WN, int KG, bool ROWS>
+__global__ __launch_bounds__(64 * WM * WN * KG) void matmul_tile_kernel(Matmul a, int tiles_m, int tiles_n, int splits)
 {
     constexpr bool EXACT = sizeof(TO) == 4;
-    using S = Tile<BM, BN, WM, WN, ROWS>;
+    using S = Tile<BM, BN, WM, WN, KG, ROWS>;
     constexpr int MT = S::MT, kRound = S::kThreads / 8;      // rows that one load of all threads brings
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = KG > 1 ? wave / (WM * WN) : 0, w = wave - group * (WM * WN);
+    const int thread = threadIdx.x - group * S::kThreads;      // of its group
     const int wm = w / WN, wn = w % WN;
     const unsigned place_of = xcd_consecutive(blockIdx.x, tiles_m * tiles_n * splits);
     const unsigned id = place_of % (tiles_m * tiles_n), split = __builtin_amdgcn_readfirstlane(place_of / (tiles_m * tiles_n));
@@ -196,12 +201,14 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int
     const long long m0 = (long long)__builtin_amdgcn_readfirstlane(8 * band + in_band % deep) * BM;      // (unsigned division is
     const long long n0 = (long long)__builtin_amdgcn_readfirstlane(in_band / deep) * BN;                 // done in the lanes)
     const int blocks = a.K / 128 + (a.K % 128 != 0), last = (a.K + 15) / 16 * 16 - 16;
-    const int k0 = (int)((long long)blocks * split / splits), nk = (int)((long long)blocks * (split + 1) / splits);      // this split's
+    // this group's blocks
+    auto from = [&](int part) { return __builtin_amdgcn_readfirstlane((int)((long long)blocks * part / (splits * KG))); };
+    const int k0 = from(split * KG + group), nk = from(split * KG + group + 1);
     const int rows_a = (int)min((long long)BM, a.M - m0), rows_b = (int)min((long long)BN, a.N - n0);
     const uint32_t lda = (uint32_t)a.lda, ldb = (uint32_t)a.ldb;
     const auto A = buffer_of(static_cast<const uint8_t *>(a.A) + m0 * a.lda, (rows_a - 1) * lda + last + 16);
     const auto B = buffer_of(static_cast<const uint8_t *>(a.B) + n0 * a.ldb, (rows_b - 1) * ldb + last + 16);
-    const int row = threadIdx.x >> 3, place = threadIdx.x & 7;
+    const int row = thread >> 3, place = thread & 7;
     const int piece_a = (place ^ (row & 7)) * 16, piece_b = (place ^ ((row & 3) | (row >> 2 & 4))) * 16;
     const uint32_t at_a = row * lda + piece_a, at_b = row * ldb + piece_b;
     // Loads lo .. hi - 1 of the kLoads that bring block kb to LDS: rows of A, rows of B, scales (64 rows a load).  Behind a
@@ -242,7 +249,7 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int
         p.set(*reinterpret_cast<const u32x4 *>(buf + at), *reinterpret_cast<const u32x4 *>(buf + (at ^ 64)));
         return p;
     };
-    auto buffer = [&](int kb) { return lds + kb % 2 * S::kBuffer; };
+    auto buffer = [&](int kb) { return lds + (KG > 1 ? group * (2 * S::kBuffer) : 0) + kb % 2 * S::kBuffer; };
     // block kb is in LDS for all wavefronts, and nobody reads the block before it any more
     auto arrive = [&](int kb) {
         __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): what this wavefront asked for is there
@@ -251,7 +258,7 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int
 #pragma unroll
             for (int i = 0; i < (BM + BN) / kRound; ++i) {
                 const int k = i < BM / kRound ? piece_a : piece_b;
-                u32x4 *q = reinterpret_cast<u32x4 *>(buffer(kb) + i * kRound * 128 + threadIdx.x * 16);
+                u32x4 *q = reinterpret_cast<u32x4 *>(buffer(kb) + i * kRound * 128 + thread * 16);
                 if (k + 16 > left) *q = keep(*q, left - k);
             }
         }
@@ -336,6 +343,26 @@ __global__ __launch_bounds__(64 * WM * WN) void matmul_tile_kernel(Matmul a, int
     };
     for (int kb = k0; kb + 1 < nk; ++kb) block(kb, std::false_type{});
     block(nk - 1, std::true_type{});
+    if constexpr (KG > 1) {
+        static_assert(KG == 2, "one group adds the other's");
+        // as many barriers in every group: they differ by a block at most
+        const int longest = max(from(split * KG + 1) - from(split * KG), from(split * KG + 2) - from(split * KG + 1));
+        if (nk - k0 < longest) __syncthreads();
+        __syncthreads();      // LDS is free
+        f32x4 *joint = reinterpret_cast<f32x4 *>(lds) + thread;
+        static_assert(S::kThreads * MT * 4 * 16 <= 2 * KG * S::kBuffer, "sums of a group in LDS");
+        if (group == 1)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) joint[(i * 4 + j) * S::kThreads] = acc[i][j];
+        __syncthreads();
+        if (group == 1) return;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] += joint[(i * 4 + j) * S::kThreads];
+    }
     const long long col = n0 + wn * 64 + 16 * g;
     const int left = (int)min(16LL, a.N - col);
     auto store = [&](auto *C, long long ldc) {
@@ -386,12 +413,13 @@ template <typename TO> __global__ __launch_bounds__(256) void matmul_join_kernel
 }
 
 // How a product is shared out: the kernel for few rows (tile -1), or tiles and splits of K.
-constexpr int kTileRows[4] = {256, 128, 64, 128}, kTileCols[4] = {256, 128, 128, 64};      // (the first: 128 rows for fp32 results)
+// (the first: 128 rows for fp32 results; the last two: two groups of wavefronts)
+constexpr int kTileRows[6] = {256, 128, 64, 128, 64, 128}, kTileCols[6] = {256, 128, 128, 64, 128, 64}, kTileGroups[6] = {1, 1, 1, 1, 2, 2};
 // cols: columns of C that it takes; what is left is a product of its own, planned by itself.
 struct Plan { int tile, splits, cols; };
 
 // The cheapest by a model of each, in us, fitted to calls on an MI355X of 256 compute units (clocks differ by some per cent from
-// card to card; what it picked was within 11 % of the best of all for 22 sizes from 65 x 4096 x 4096 to 8192 x 64 x 4096):
+// card to card; what it picked was within 8 % of the best of all for 17 sizes from 32 x 20544 x 4096 to 8192 x 64 x 4096, either type):
 //   tiles      rounds of as many workgroups as a compute unit holds, each 1.5 us and so much a block of K, by how many
 //              share a compute unit; splits add the join: 4 us and their sums to memory and back
 //   few rows   B at 5 TB/s and the rows of A, read for every 16 rows of B, at 12 TB/s
@@ -400,17 +428,18 @@ struct Plan { int tile, splits, cols; };
 Plan plan_of(int M, int N, int K, bool exact, double *cost = nullptr)
 {
     // us a block of K of 1, 2, 3 workgroups a compute unit
-    static constexpr double kBlock[2][4][3] = {{{1.5}, {0.95, 1.28}, {0.72, 0.83, 1.15}, {0.72, 0.83, 1.15}},
-                                               {{1.75}, {1.55, 2.3}, {0.93, 1.35, 2.0}, {0.93, 1.35, 2.0}}};
-    static constexpr int kHeld[4] = {1, 2, 3, 3};
+    static constexpr double kBlock[2][6][3] = {{{1.5}, {0.95, 1.28}, {0.72, 0.83, 1.15}, {0.72, 0.83, 1.15}, {0.83}, {0.83}},
+                                               {{1.75}, {1.55, 2.3}, {0.93, 1.35, 2.0}, {0.93, 1.35, 2.0}, {1.35}, {1.35}}};
+    static constexpr int kHeld[6] = {1, 2, 3, 3, 1, 1};
     const int blocks = K / 128 + (K % 128 != 0), cus = device_cu_count();
     Plan best = {0, 1, N};
     double least = 1e30;
     auto consider = [&](int t, int N, double besides) {
         const int rows = t == 0 && exact ? 128 : kTileRows[t];
         const double tiles = (double)((M + (long long)rows - 1) / rows) * (double)((N + (long long)kTileCols[t] - 1) / kTileCols[t]);
-        for (int s = 1; s <= 8 && (s == 1 || 2 * s <= blocks); s *= 2) {
-            const double groups = tiles * s, each = (double)((blocks + s - 1) / s), full = (double)((long long)(groups / (cus * kHeld[t])));
+        for (int s = 1; s <= 8 && (s * kTileGroups[t] == 1 || 2 * s * kTileGroups[t] <= blocks); s *= 2) {
+            const int parts = s * kTileGroups[t];
+            const double groups = tiles * s, each = (double)((blocks + parts - 1) / parts), full = (double)((long long)(groups / (cus * kHeld[t])));
             const int more = (int)((groups - full * cus * kHeld[t] + cus - 1) / cus);      // a compute unit in the last round
             double us = 3 + full * (each * kBlock[exact][t][kHeld[t] - 1] + 1.5);
             if (more > 0) us += each * kBlock[exact][t][more - 1] + 1.5;
@@ -419,7 +448,7 @@ Plan plan_of(int M, int N, int K, bool exact, double *cost = nullptr)
             if (us < least) least = us, best = {t, s, N};
         }
     };
-    for (int t = 0; t < 4; ++t) consider(t, N, 0);
+    for (int t = 0; t < 6; ++t) consider(t, N, 0);
     const int rest = N % kTileCols[0];
     if (rest > 0 && rest <= kTileCols[0] / 4 && N > rest) {
         double more = 0;
@@ -468,16 +497,16 @@ hipError_t launch_matmul(const Matmul &whole, bool bf16_out, hipStream_t stream)
             else rows(integral_constant<int, 4>{}, integral_constant<int, 1>{});
             return;
         }
-        auto tile = [&](auto by_rows, auto bm, auto bn, auto wm, auto wn) {
-            constexpr int BM = bm.value, BN = bn.value, WM = wm.value, WN = wn.value;
-            using S = Tile<BM, BN, WM, WN, by_rows.value>;
-            auto kernel = matmul_tile_kernel<TO, BM, BN, WM, WN, by_rows.value>;
+        auto tile = [&](auto by_rows, auto bm, auto bn, auto wm, auto wn, auto kg) {
+            constexpr int BM = bm.value, BN = bn.value, WM = wm.value, WN = wn.value, KG = kg.value;
+            using S = Tile<BM, BN, WM, WN, KG, by_rows.value>;
+            auto kernel = matmul_tile_kernel<TO, BM, BN, WM, WN, KG, by_rows.value>;
             static std::atomic<uint64_t> armed{0};
-            const size_t bytes = 2 * S::kBuffer;
+            const size_t bytes = 2 * KG * S::kBuffer;
             status = arm_dynamic_lds(armed, reinterpret_cast<const void *>(kernel), bytes);
             if (status != hipSuccess) return;
             const int tm = (int)((a.M + (long long)BM - 1) / BM), tn = (int)((a.N + (long long)BN - 1) / BN);
-            hipLaunchKernelGGL(kernel, dim3((unsigned)tm * (unsigned)tn * p.splits), dim3(S::kThreads), bytes, stream, a, tm, tn, p.splits);
+            hipLaunchKernelGGL(kernel, dim3((unsigned)tm * (unsigned)tn * p.splits), dim3(S::kThreads * KG), bytes, stream, a, tm, tn, p.splits);
         };
         auto which = [&](auto by_rows) {
             using std::integral_constant;
@@ -487,10 +516,12 @@ hipError_t launch_matmul(const Matmul &whole, bool bf16_out, hipStream_t stream)
             integral_constant<int, 64> c64;
             integral_constant<int, 128> c128;
             integral_constant<int, 256> c256;
-            if (p.tile == 0) tile(by_rows, integral_constant<int, EXACT ? 128 : kTileRows[0]>{}, c256, c2, c4);
-            else if (p.tile == 1) tile(by_rows, c128, c128, c2, c2);
-            else if (p.tile == 2) tile(by_rows, c64, c128, c2, c2);
-            else tile(by_rows, c128, c64, c4, c1);
+            if (p.tile == 0) tile(by_rows, integral_constant<int, EXACT ? 128 : kTileRows[0]>{}, c256, c2, c4, c1);
+            else if (p.tile == 1) tile(by_rows, c128, c128, c2, c2, c1);
+            else if (p.tile == 2) tile(by_rows, c64, c128, c2, c2, c1);
+            else if (p.tile == 3) tile(by_rows, c128, c64, c4, c1, c1);
+            else if (p.tile == 4) tile(by_rows, c64, c128, c2, c2, c2);
+            else tile(by_rows, c128, c64, c4, c1, c2);
         };
         if (a.b_rows == 1) which(std::true_type{});
         else which(std::false_type{});
