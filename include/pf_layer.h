@@ -132,7 +132,8 @@ pf_status pf_matmul_fp8(const void *A, long long lda, const float *sa, const voi
  *                                                   NULL when that is 0, as for L up to 16; the forward and the
  *                                                   backward need the same)
  *
- * L == 0: hL receives h0 (or zeros), the sequence pointers may be NULL.  B == 0: nothing is done.
+ * L == 0: hL receives h0 (or zeros), the sequence pointers may be NULL.  B == 0: nothing is done.  L up to 2^30
+ * (PF_ERR_UNSUPPORTED).
  * Where h overflows to infinity, later values may be NaN instead of infinite.
  */
 typedef enum { PF_GATE_VALUE = 0, PF_GATE_LOG = 1, PF_GATE_LOGIT = 2 } pf_gate;

@@ -97,7 +97,7 @@ namespace {
 pf_status gated_checks(int B, int L, int D, pf_gate gate, pf_dtype dt)
 {
     if (B < 0 || L < 0 || D <= 0) return PF_ERR_SHAPE;
-    if (!known(dt) || (gate != PF_GATE_VALUE && gate != PF_GATE_LOG && gate != PF_GATE_LOGIT)) return PF_ERR_UNSUPPORTED;
+    if (L > 1 << 30 || !known(dt) || (gate != PF_GATE_VALUE && gate != PF_GATE_LOG && gate != PF_GATE_LOGIT)) return PF_ERR_UNSUPPORTED;
     return PF_OK;
 }
 pf_status gated_workspace(int B, int L, int D, pf_dtype dt, const void *workspace, size_t workspace_bytes)

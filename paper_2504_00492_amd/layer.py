@@ -3,11 +3,12 @@ binding.py: every step of the computation runs in the HIP kernels of libpf_layer
 stream, and without the library this module raises.
 
 The functions without the pf_ prefix take torch tensors on the GPU, check them, allocate the outputs (and a workspace unless
-one is handed in) and make one library call on the current stream of the tensors' device, or on `stream`.
+one is handed in) and make one library call on the current stream of the tensors' device, or on `stream`, which all of them take.
 """
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -206,19 +207,35 @@ def _workspace(need, given, device):
     return given, given.data_ptr(), given.numel() * given.element_size()
 
 
-def _call(fn, name, index, stream, *args):
-    """One library call with the tensors' device as the current one, on its current stream unless one is given."""
-    stream = _stream(index) if stream is None else _stream_handle(stream)
+def _call(fn, name, index, *args):
+    """One library call on the current stream of the tensors' device, with that device as the current one."""
     if _current() == index:
-        st = fn(*args, stream)
+        st = fn(*args, _stream(index))
     else:
         with torch.cuda.device(index):
-            st = fn(*args, stream)
+            st = fn(*args, _stream(index))
     if st != PF_OK:
         raise PfError(st, name)
 
 
-def norm_fwd(X, w=None, R=None, *, eps, y: bool = True, fp8: bool = False, inplace: bool = False, stream=None):
+def _on_stream(f):
+    """f with an argument `stream` (a torch stream, or the handle of one; None: the current one).  The call's outputs and workspace
+    come from that stream's memory, as if it had been made current: memory of another stream could still be in use there,
+    or be handed out again there before the call is through."""
+    @functools.wraps(f)
+    def with_stream(*args, stream=None, **kwargs):
+        if stream is None:
+            return f(*args, **kwargs)
+        if isinstance(stream, int):
+            device = next(t for t in args if t is not None).device
+            stream = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
+        with torch.cuda.stream(stream):
+            return f(*args, **kwargs)
+    return with_stream
+
+
+@_on_stream
+def norm_fwd(X, w=None, R=None, *, eps, y: bool = True, fp8: bool = False, inplace: bool = False):
     """Root-mean-square norm of the rows of X + R (pf_norm_fwd).  X, R [M, D] (float32 or bfloat16, rows may lie apart), w [D]
     of the same type.  Returns (S, Y, Q, scale): S the stored sum (X itself without R; R's own memory with inplace, which
     asks for a contiguous R), Y the norm (None with y=False), Q and scale the norm in 8 bits (None unless fp8)."""
@@ -246,11 +263,12 @@ def norm_fwd(X, w=None, R=None, *, eps, y: bool = True, fp8: bool = False, inpla
     if fp8:
         Q, scale = _byte_rows(M, D, device), _empty((-(-D // 128), M), dtype=_F32, device=device)
         qp, cp = Q.data_ptr(), scale.data_ptr()
-    _call(_lib.pf_norm_fwd, "pf_norm_fwd", index, stream, xp, ldx, rp, ldr, wp, sp, yp, qp, -(-D // 16) * 16, cp, M, D, eps, dt)
+    _call(_lib.pf_norm_fwd, "pf_norm_fwd", index, xp, ldx, rp, ldr, wp, sp, yp, qp, -(-D // 16) * 16, cp, M, D, eps, dt)
     return S, Y, Q, scale
 
 
-def norm_bwd(S, dY, w=None, dS=None, *, eps, want_dw: bool = True, workspace=None, stream=None):
+@_on_stream
+def norm_bwd(S, dY, w=None, dS=None, *, eps, want_dw: bool = True, workspace=None):
     """Backward of norm_fwd (pf_norm_bwd): S the stored sum, dY the gradient of the norm, dS that of the sum past the norm
     (None: none).  Returns (dX, dw): dX [M, D] in the inputs' type, dw [D] in float32 (None unless wanted)."""
     dt, index = _first(S, "S", 2)
@@ -267,11 +285,12 @@ def norm_bwd(S, dY, w=None, dS=None, *, eps, want_dw: bool = True, workspace=Non
         dw = _empty(D, dtype=_F32, device=device)
         dp = dw.data_ptr()
         keep, kp, kb = _workspace(_lib.pf_norm_bwd_workspace_bytes(M, D) if workspace is None else 0, workspace, device)
-    _call(_lib.pf_norm_bwd, "pf_norm_bwd", index, stream, sp, lds, wp, yp, ldy, rp, ldr, dX.data_ptr(), dp, M, D, eps, dt, kp, kb)
+    _call(_lib.pf_norm_bwd, "pf_norm_bwd", index, sp, lds, wp, yp, ldy, rp, ldr, dX.data_ptr(), dp, M, D, eps, dt, kp, kb)
     return dX, dw
 
 
-def quant_fp8(X, *, rows: int = 1, plain: bool = True, transposed: bool = False, stream=None):
+@_on_stream
+def quant_fp8(X, *, rows: int = 1, plain: bool = True, transposed: bool = False):
     """X [M, K] (float32 or bfloat16, rows may lie apart) in 8 bits (pf_quant_fp8), with a scale for each row and 128 columns
     (rows=1) or each 128 x 128 (rows=128).  Returns (Q, scale, QT, scaleT); Q and scale are None with plain=False, QT and
     scaleT (the transposed matrix, its blocks along its own rows) unless transposed."""
@@ -292,11 +311,12 @@ def quant_fp8(X, *, rows: int = 1, plain: bool = True, transposed: bool = False,
         QT = _byte_rows(K, M, device)
         scaleT = _empty((-(-M // 128), K if rows == 1 else -(-K // 128)), dtype=_F32, device=device)
         tp, up = QT.data_ptr(), scaleT.data_ptr()
-    _call(_lib.pf_quant_fp8, "pf_quant_fp8", index, stream, xp, ldx, qp, -(-K // 16) * 16, sp, tp, -(-M // 16) * 16, up, M, K, rows, dt)
+    _call(_lib.pf_quant_fp8, "pf_quant_fp8", index, xp, ldx, qp, -(-K // 16) * 16, sp, tp, -(-M // 16) * 16, up, M, K, rows, dt)
     return Q, scale, QT, scaleT
 
 
-def matmul_fp8(A, sa, B, sb, *, b_rows: int = 128, out_dtype=_BF, workspace=None, stream=None):
+@_on_stream
+def matmul_fp8(A, sa, B, sb, *, b_rows: int = 128, out_dtype=_BF, workspace=None):
     """C [M, N] = A [M, K] times B [N, K] transposed, both e4m3 with scales (pf_matmul_fp8): sa [ceil(K/128), M], sb
     [ceil(K/128), N] (b_rows=1) or [ceil(K/128), ceil(N/128)] (b_rows=128).  Rows of A and B lie a multiple of 16 bytes apart,
     as quant_fp8 and norm_fwd lay them.  out_dtype: bfloat16 or float32."""
@@ -320,7 +340,7 @@ def matmul_fp8(A, sa, B, sb, *, b_rows: int = 128, out_dtype=_BF, workspace=None
     C = _empty((M, N), dtype=out_dtype, device=device)
     # (16 rows at most never need a workspace)
     keep, kp, kb = _workspace(_lib.pf_matmul_fp8_workspace_bytes(M, N, K, b_rows) if workspace is None and M > 16 else 0, workspace, device)
-    _call(_lib.pf_matmul_fp8, "pf_matmul_fp8", index, stream, ap, lda, sap, bp, ldb, sbp, b_rows, C.data_ptr(), N, M, N, K, dt, kp, kb)
+    _call(_lib.pf_matmul_fp8, "pf_matmul_fp8", index, ap, lda, sap, bp, ldb, sbp, b_rows, C.data_ptr(), N, M, N, K, dt, kp, kb)
     return C
 
 
@@ -330,7 +350,8 @@ def _gate_of(gate):
     return GATES[gate]
 
 
-def gated_fwd(X, G, h0=None, *, gate: str = "log", mix: bool = False, workspace=None, stream=None):
+@_on_stream
+def gated_fwd(X, G, h0=None, *, gate: str = "log", mix: bool = False, workspace=None):
     """The gated linear recurrence h_t = a_t h_{t-1} + b_t (pf_gated_fwd): a = G, exp(G) or its sigmoid by gate ("value",
     "log", "logit"), b = X, or (1 - a) X with mix.  X, G [B, L, D] (float32 or bfloat16, tokens and sequences may lie apart or in the
     other order), h0 [B, D] float32 or None.  Returns (Y [B, L, D], h_L [B, D] float32)."""
@@ -344,11 +365,12 @@ def gated_fwd(X, G, h0=None, *, gate: str = "log", mix: bool = False, workspace=
     Y, hL = _same(X), _empty((B, D), dtype=_F32, device=device) if h0 is None else _like(h0)
     # (16 tokens at most never need a workspace)
     keep, kp, kb = _workspace(_lib.pf_gated_workspace_bytes(B, L, D, dt) if workspace is None and L > 16 else 0, workspace, device)
-    _call(_lib.pf_gated_fwd, "pf_gated_fwd", index, stream, *x, *g, hp, Y.data_ptr(), hL.data_ptr(), B, L, D, form, bool(mix), dt, kp, kb)
+    _call(_lib.pf_gated_fwd, "pf_gated_fwd", index, *x, *g, hp, Y.data_ptr(), hL.data_ptr(), B, L, D, form, bool(mix), dt, kp, kb)
     return Y, hL
 
 
-def gated_bwd(X, G, Y, dY, h0=None, dhL=None, *, gate: str = "log", mix: bool = False, workspace=None, stream=None):
+@_on_stream
+def gated_bwd(X, G, Y, dY, h0=None, dhL=None, *, gate: str = "log", mix: bool = False, workspace=None):
     """Backward of gated_fwd (pf_gated_bwd) from what it was given and returned (X may be None without mix), dY the gradient of
     Y, dhL that of h_L (float32, None: none).  Returns (dX, dG, dh0)."""
     dt, index = _first(G, "G", 3)
@@ -365,6 +387,6 @@ def gated_bwd(X, G, Y, dY, h0=None, dhL=None, *, gate: str = "log", mix: bool = 
     dX, dG = _same(G), _same(G)
     dh0 = _empty((B, D), dtype=_F32, device=device) if h0 is None else _like(h0)
     keep, kp, kb = _workspace(_lib.pf_gated_workspace_bytes(B, L, D, dt) if workspace is None and L > 16 else 0, workspace, device)
-    _call(_lib.pf_gated_bwd, "pf_gated_bwd", index, stream, *x, *g, hp, yp, *dy, ep, dX.data_ptr(), dG.data_ptr(), dh0.data_ptr(), B, L, D,
+    _call(_lib.pf_gated_bwd, "pf_gated_bwd", index, *x, *g, hp, yp, *dy, ep, dX.data_ptr(), dG.data_ptr(), dh0.data_ptr(), B, L, D,
           form, bool(mix), dt, kp, kb)
     return dX, dG, dh0

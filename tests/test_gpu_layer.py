@@ -525,6 +525,25 @@ def test_the_same_bits_again_and_on_another_stream(layer):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_stream_argument(layer):
+    """`stream` (a stream or its handle) is where the call runs and whose memory it takes: work queued on the current stream, which
+    still uses memory that is freed at once, is not disturbed, and the result does not wait for it."""
+    x, g = rnd(1, 2, 4000, 256, dt=BF).cuda(), gates(2, 2, 4000, 256, "log", BF).cuda()
+    want = layer.gated_fwd(x, g)
+    back = layer.gated_bwd(None, g, want[0], x)
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    for stream in (other, other.cuda_stream, torch.cuda.default_stream().cuda_stream):
+        busy = torch.zeros(1 << 22, device="cuda")
+        for _ in range(50):
+            busy = busy + 1
+        got = layer.gated_fwd(x, g, stream=stream)
+        grads = layer.gated_bwd(None, g, want[0], x, stream=stream)
+        torch.cuda.synchronize()
+        assert (busy == 50).all()
+        assert all(torch.equal(a, b) for a, b in zip((*got, *grads), (*want, *back)))
+
+
 def test_in_a_graph(layer):
     """Captured once, replayed with eager work between: every replay gives the eager bits."""
     go = _calls(layer)

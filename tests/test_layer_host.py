@@ -95,7 +95,7 @@ NULL, SHAPE, UNSUPPORTED, ALIGN, WORKSPACE = 1, 2, 3, 4, 5
     (_matmul, dict(B=P + 8), ALIGN), (_matmul, dict(C=P + 2), ALIGN),
     (_gated_fwd, dict(X=None), NULL), (_gated_fwd, dict(G=None), NULL), (_gated_fwd, dict(Y=None), NULL),
     (_gated_fwd, dict(B=-1), SHAPE), (_gated_fwd, dict(L=-1), SHAPE), (_gated_fwd, dict(D=0), SHAPE), (_gated_fwd, dict(xt=-8), SHAPE),
-    (_gated_fwd, dict(gate=3), UNSUPPORTED), (_gated_fwd, dict(dt=2), UNSUPPORTED), (_gated_fwd, dict(h0=P + 4), ALIGN),
+    (_gated_fwd, dict(gate=3), UNSUPPORTED), (_gated_fwd, dict(L=(1 << 30) + 1), UNSUPPORTED), (_gated_fwd, dict(dt=2), UNSUPPORTED), (_gated_fwd, dict(h0=P + 4), ALIGN),
     (_gated_bwd, dict(X=None), NULL), (_gated_bwd, dict(Y=None), NULL), (_gated_bwd, dict(dY=None), NULL),
     (_gated_bwd, dict(dG=None), NULL), (_gated_bwd, dict(dyb=-1), SHAPE), (_gated_bwd, dict(gate=-1), UNSUPPORTED),
     (_gated_bwd, dict(dX=P + 2), ALIGN), (_gated_fwd, dict(G=P + 1), ALIGN)])
