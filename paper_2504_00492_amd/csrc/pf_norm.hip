@@ -61,7 +61,10 @@ __global__ __launch_bounds__(kThreads<G>) void norm_fwd_kernel(NormFwd a)
     if (a.w)
 #pragma unroll
         for (int i = 0; i < NV; ++i) w[i] = load8<T, VEC>(static_cast<const T *>(a.w) + col(i), a.D - col(i));
-    for (long long row = (long long)blockIdx.x * rows + threadIdx.x / G; row < a.M; row += (long long)gridDim.x * rows) {
+    // 16 neighbouring rows on one XCD: a block's scales of neighbouring rows lie side by side, and meet in its L2 (32768 rows of 4096:
+    // 407 MB written instead of 441; all of an XCD's rows side by side write as little, but 189 us instead of 176)
+    const unsigned b = blockIdx.x, first = (b | 127) < gridDim.x ? (b & ~127u) | (b & 7) << 4 | (b >> 3 & 15) : b;
+    for (long long row = (long long)first * rows + threadIdx.x / G; row < a.M; row += (long long)gridDim.x * rows) {
         Raw8<T, VEC> x[NV], r[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) x[i] = load8<T, VEC>(X + row * a.ldx + col(i), a.D - col(i));
