@@ -6,6 +6,10 @@
 // below that (measured: 1.4e-5 of the result's norm for normally distributed values), 1/100 of what the rounding to bf16 costs.
 // C in fp32: the values are turned to bf16, which holds every e4m3 number, and go through v_mfma_f32_16x16x32_bf16, whose sums are
 // fp32 ones (7e-9 of the norm), four of them to a block.
+// 8192 x 8192 x 8192 into bf16: 450 us, 2450 TFLOP/s, 89 % of what the library's product of 8-bit matrices without scales reaches
+// (2765), and 405 us with the scales left out, so they cost 10 %; the matrix units are busy 63 % of the time at the 1.87 GHz that the
+// card's power then allows.  Into fp32, a scale for every row of both: 4096 x 4096 x 8192 254 us, 1080 TFLOP/s, bound by turning the
+// values to bf16 in the vector units (the library's bf16 product: 1390).  Three rows of A, 20544 x 4096: 19.9 us, 4.2 TB/s.
 // A lane (r = l & 15, g = l >> 4) holds 32 values of row r of either operand; which 32 does not matter as long as both
 // agree: the 16 bytes from 16 g on and from 64 + 16 g on.  B's rows are the first operand and A's the second, so that a lane's four
 // results, rows 4 g .. 4 g + 3 of column r, lie side by side in C.
