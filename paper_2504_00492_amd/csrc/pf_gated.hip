@@ -9,17 +9,17 @@
 // Three kernels: a few tokens, a lane through all of them; many sequences and channels, a workgroup along a chain (64 V
 // channels of one sequence) from tile to tile; else every tile has a workgroup.  A tile tells the (A, H) of its channels as soon as
 // it has read them, looks back for the nearest tile in front whose outgoing values are told (each of its wavefronts listens to one
-// of the eight in front), runs these through the (A, H) of the tiles between, and tells its own outgoing values.  A word that is told
-// stands for itself (clear is a pattern that no value has), 8 bytes in one store, so no fence orders anything.  Tiles are handed out by
-// a counter, all chains' first tiles first: a workgroup waits only for tiles handed out before its own, whose workgroups are on the
-// chip already and wait for nothing later, so every wait ends.  What a tile makes of the values that come in depends on the tiles between
-// them in order, whichever were told, so the bits do not depend on timing.
+// of the eight in front, where there are few chains to two of sixteen), runs these through the (A, H) of the tiles between, and tells
+// its own outgoing values.  A word that is told stands for itself (clear is a pattern that no value has), 8 bytes in one store, so no
+// fence orders anything.  Tiles are handed out by a counter, all chains' first tiles first: a workgroup waits only for tiles handed
+// out before its own, whose workgroups are on the chip already and wait for nothing later, so every wait ends.  What a tile makes of
+// the values that come in depends on the tiles between them in order, whichever were told, so the bits do not depend on timing.
 //
 // Bound by HBM: 1 x 65536 x 4096 forward in bf16 321 us, 5.0 TB/s (a plain copy: 5.1); 1 x 65536 x 2048 in fp32 5.5 TB/s; backward with
 // the mix 2 x 8192 x 4096 183 us, 4.4 TB/s, where the tiles are not long enough for what a tile waits to be hidden.  A long sequence of few
-// channels is bound by the chain, 0.2 us a tile: 1 x 65536 x 64 79 us.  Tried and left: two channels more to a lane (321 -> 375 us), workgroups
-// that draw tile after tile and read ahead (475: what they hold in registers makes tiles short), 16 tiles listened to (twice the words
-// to read: 431), four or twelve wavefronts (363, 348).
+// channels is bound by the chain, 0.18 us a tile: 1 x 65536 x 64 62 us.  Tried and left: two channels more to a lane (321 -> 375 us), workgroups
+// that draw tile after tile and read ahead (475: what they hold in registers makes tiles short), 16 tiles listened to here too (twice the words
+// to read: 351), four or twelve wavefronts (363, 348).
 #include "pf_layer_common.h"
 #include "pf_layer_internal.h"
 
@@ -332,14 +332,14 @@ __device__ __forceinline__ void gated_walk(const Gated &a, int groups, Pair (&sp
 }
 
 // A workgroup for each tile.
-template <int V> struct TileLds {
-    Pair spans[kWaves][V][64], behind[kWaves][V][64];
-    float outs[kWaves][V][64];
-    int heard[kWaves];      // of a tile in front: 1 its (A, H), 2 what goes out of it
+template <int V, int PER> struct TileLds {
+    Pair spans[kWaves][V][64], behind[kWaves * PER][V][64];
+    float outs[kWaves * PER][V][64];
+    int heard[kWaves * PER];      // of a tile in front: 1 its (A, H), 2 what goes out of it
     uint32_t ticket;
 };
-template <typename K>
-__device__ __forceinline__ void gated_tile(const Gated &a, int groups, int chains, int tiles, const Work &work, TileLds<K::V> &lds)
+template <typename K, int PER>
+__device__ __forceinline__ void gated_tile(const Gated &a, int groups, int chains, int tiles, const Work &work, TileLds<K::V, PER> &lds)
 {
     using T = typename K::T;
     constexpr int V = K::V;
@@ -375,37 +375,41 @@ __device__ __forceinline__ void gated_tile(const Gated &a, int groups, int chain
     float in[V];
     if (tile == 0) {
         c.incoming(in);
-    } else {      // each wavefront listens to one of the tiles in front
-        const long long there = at - (long long)min(w + 1, tile) * row;
-        bool has_out = false, has_span = false;
+    } else {      // each wavefront listens to PER of the tiles in front
+        bool has_out[PER] = {}, has_span[PER] = {};
         int from;
         while (true) {
-            if (!has_span && w < tile - 1) {      // (the first tile only tells what goes out)
-                bool ready = true;
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const unsigned long long p = hear(work.span + there + 64 * v + (unsigned)lane);
-                    ready = ready && (uint32_t)p != kClear;
-                    lds.behind[w][v][lane] = {__uint_as_float((uint32_t)p), __uint_as_float((uint32_t)(p >> 32))};
-                }
-                has_span = __all(ready);
-            }
-            if (!has_out && w < tile) {
-                bool ready = true;
+            for (int q = 0; q < PER; ++q) {
+                const int k = q * kWaves + w;
+                const long long there = at - (long long)min(k + 1, tile) * row;
+                if (!has_span[q] && k < tile - 1) {      // (the first tile only tells what goes out)
+                    bool ready = true;
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const uint32_t o = hear(work.out + there + 64 * v + (unsigned)lane);
-                    ready = ready && o != kClear;
-                    lds.outs[w][v][lane] = __uint_as_float(o);
+                    for (int v = 0; v < V; ++v) {
+                        const unsigned long long p = hear(work.span + there + 64 * v + (unsigned)lane);
+                        ready = ready && (uint32_t)p != kClear;
+                        lds.behind[k][v][lane] = {__uint_as_float((uint32_t)p), __uint_as_float((uint32_t)(p >> 32))};
+                    }
+                    has_span[q] = __all(ready);
                 }
-                has_out = __all(ready);
+                if (!has_out[q] && k < tile) {
+                    bool ready = true;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        const uint32_t o = hear(work.out + there + 64 * v + (unsigned)lane);
+                        ready = ready && o != kClear;
+                        lds.outs[k][v][lane] = __uint_as_float(o);
+                    }
+                    has_out[q] = __all(ready);
+                }
+                if (lane == 0) lds.heard[k] = (has_span[q] ? 1 : 0) | (has_out[q] ? 2 : 0);
             }
-            if (lane == 0) lds.heard[w] = (has_span ? 1 : 0) | (has_out ? 2 : 0);
             __syncthreads();
             from = -1;      // the nearest tile whose outgoing values are told, if all between have told their (A, H)
             bool open = true;
 #pragma unroll
-            for (int k = 0; k < kWaves; ++k) {
+            for (int k = 0; k < kWaves * PER; ++k) {
                 const int h = lds.heard[k];
                 if (open && (h & 2)) from = k, open = false;
                 open = open && (h & 1);
@@ -471,14 +475,14 @@ __global__ __launch_bounds__(64 * kWaves) void gated_walk_kernel(Gated a, int gr
     by_form<T, V, VEC, BACK, MIX>(a.gate, [&](auto k) { gated_walk<decltype(k)>(a, groups, spans); });
 }
 // (so many wavefronts to a SIMD; where channels lie at odd places their registers allow three)
-template <typename T, int V, bool VEC, bool BACK, bool MIX>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(!VEC ? 3 : BACK ? 6 : 4)))
+template <typename T, int V, bool VEC, bool BACK, bool MIX, int PER>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(!VEC ? 3 : BACK && PER == 1 ? 6 : 4)))
 void gated_tile_kernel(Gated a, int groups, int chains, int tiles, Work work)
 {
-    __shared__ TileLds<V> lds;
+    __shared__ TileLds<V, PER> lds;
     if (threadIdx.x == 0) lds.ticket = __hip_atomic_fetch_add(work.next, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1u;
     __syncthreads();
-    by_form<T, V, VEC, BACK, MIX>(a.gate, [&](auto k) { gated_tile<decltype(k)>(a, groups, chains, tiles, work, lds); });
+    by_form<T, V, VEC, BACK, MIX>(a.gate, [&](auto k) { gated_tile<decltype(k), PER>(a, groups, chains, tiles, work, lds); });
 }
 template <typename T, int V, bool VEC, bool BACK, bool MIX> __global__ __launch_bounds__(64) void gated_few_kernel(Gated a, int groups)
 {
@@ -488,6 +492,7 @@ template <typename T, int V, bool VEC, bool BACK, bool MIX> __global__ __launch_
 enum { kFew, kWalk, kTiles };
 struct Plan {
     int how, groups, chains, tiles;
+    bool farther;
     size_t bytes;
 };
 Plan plan(int B, int L, int D, bool is_bf16, bool back)
@@ -499,6 +504,9 @@ Plan plan(int B, int L, int D, bool is_bf16, bool back)
     const int tile = is_bf16 ? tile_tokens<bf16>(back) : tile_tokens<float>(back);
     p.tiles = L / tile + (L % tile != 0);
     p.how = L <= 16 ? kFew : L <= 2 * kWaves * kWalkSteps || p.chains >= 4 * device_cu_count() ? kWalk : kTiles;
+    // Few chains have many of their tiles on the chip at once, and listening to sixteen of them makes a step of the chain longer: 1 x 65536
+    // channels in bf16, forward 64: 77 -> 62 us, 512: 92 -> 76, 1024: 107 -> 110; backward 64: 188 -> 144, 1024: 234 -> 198, 2048: 316 -> 356.
+    p.farther = p.tiles > 2 * kWaves && p.chains <= (back ? 8 : 6);
     if (p.how == kTiles) p.bytes = 256 + (size_t)p.tiles * p.chains * (64 * V) * 12;
     return p;
 }
@@ -524,8 +532,9 @@ template <bool BACK> hipError_t launch(const Gated &a, bool is_bf16, bool aligne
             work.span = reinterpret_cast<unsigned long long *>(base + 256);
             work.out = reinterpret_cast<uint32_t *>(base + 256 + words * 8);
             const long long count = (long long)p.chains * p.tiles;
-            hipLaunchKernelGGL((gated_tile_kernel<T, V, vec.value, BACK, mix.value>), dim3((unsigned)count),
-                               dim3(64 * kWaves), 0, stream, a, p.groups, p.chains, p.tiles, work);
+            auto kernel = p.farther ? gated_tile_kernel<T, V, vec.value, BACK, mix.value, 2>
+                                    : gated_tile_kernel<T, V, vec.value, BACK, mix.value, 1>;
+            hipLaunchKernelGGL(kernel, dim3((unsigned)count), dim3(64 * kWaves), 0, stream, a, p.groups, p.chains, p.tiles, work);
         }
     };
     auto with = [&](auto one, auto vec) {

@@ -448,6 +448,29 @@ def test_gated_packed_sequences(layer, L, dt):
         assert (got[1][:, cut] == 0).all()
 
 
+FEW_CHAINS = [(1, 6000, 33), (2, 5500, 131), (1, 4099, 768), (1, 3500, 1030)]
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("B,L,D", FEW_CHAINS)
+def test_gated_few_chains(layer, B, L, D, dt):
+    """Long sequences of few channels against the formula, and bit for bit against the same ones among many."""
+    x, g, h0, y, dy, dh = (rnd(1, B, L, D, dt=dt), gates(2, B, L, D, "log", dt), rnd(3, B, D), rnd(4, B, L, D, dt=dt), rnd(5, B, L, D, dt=dt),
+                           rnd(6, B, D))
+    ref, tol = gated_ref(x, g, h0, "log", True)
+    Y, hL = layer.gated_fwd(x.cuda(), g.cuda(), h0.cuda(), mix=True)
+    near(Y, ref, tol + HALF[dt] * ref.abs())
+    near(hL, ref[:, -1], tol[:, -1])
+    back = layer.gated_bwd(x.cuda(), g.cuda(), y.cuda(), dy.cuda(), h0.cuda(), dh.cuda(), mix=True)
+    for out, (r, t), half in zip(back, gated_grads(x, g, h0, y, dy, dh, "log", True), (HALF[dt], HALF[dt], 0)):
+        near(out, r, t + half * r.abs())
+    many = lambda t: t.repeat(12, *[1] * (t.dim() - 1)).cuda()  # noqa: E731
+    for one, all_ in zip((Y, hL), layer.gated_fwd(many(x), many(g), many(h0), mix=True)):
+        assert torch.equal(all_, one.repeat(12, *[1] * (one.dim() - 1)))
+    for one, all_ in zip(back, layer.gated_bwd(many(x), many(g), many(y), many(dy), many(h0), many(dh), mix=True)):
+        assert torch.equal(all_, one.repeat(12, *[1] * (one.dim() - 1)))
+
+
 @pytest.mark.parametrize("L", [40, 3000])
 def test_gated_special_values(layer, L):
     """NaN stays in its channel and sequence and reaches no earlier token; gates above one that overflow a span's product."""
