@@ -34,8 +34,11 @@ constexpr int kWaves = 8, kWalkSteps = 16;
 // Steps of a wavefront's span of a tile, as its registers allow: forward (two arrays) two workgroups to a compute unit, of tiles that are
 // long, so that there is less to tell and to wait for (1 x 65536 x 4096, bf16: 16 steps 351 us, 24 320); backward (up to four
 // arrays) three of short ones (2 x 8192 x 4096: two of 16 steps 188 us, three of 9 183; 16 x 2048 x 4096 316 and 314).
-template <typename T, bool BACK> constexpr int kTileSteps = BACK ? 9 : sizeof(T) == 2 ? 24 : 32;
-template <typename T> inline int tile_tokens(bool back) { return kWaves * (back ? kTileSteps<T, true> : kTileSteps<T, false>); }
+template <typename T, bool BACK, bool FARTHER = false> constexpr int kTileSteps = BACK ? (FARTHER ? 16 : 9) : sizeof(T) == 2 ? 24 : 32;
+template <typename T> inline int tile_tokens(bool back, bool farther)
+{
+    return kWaves * (!back ? kTileSteps<T, false> : farther ? kTileSteps<T, true, true> : kTileSteps<T, true>);
+}
 
 // the decay a, 1 - a, and d a / d g of a gate's value
 struct Gate { float a, rest, slope; };
@@ -347,7 +350,7 @@ __device__ __forceinline__ void gated_tile(const Gated &a, int groups, int chain
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t id = __builtin_amdgcn_readfirstlane(lds.ticket);
     const int tile = __builtin_amdgcn_readfirstlane(id / chains), chain = (int)id - tile * chains;      // (unsigned division is done in the lanes)
-    constexpr int steps = kTileSteps<T, K::BACK>;
+    constexpr int steps = kTileSteps<T, K::BACK, (PER > 1)>;
     const int mine = (tile * kWaves + w) * steps;
     const Chain<T, V, VEC, K::BACK> c(a, chain, groups, lane);
     Span<K, steps> s;
@@ -501,12 +504,17 @@ Plan plan(int B, int L, int D, bool is_bf16, bool back)
     Plan p = {};
     p.groups = (D + 64 * V - 1) / (64 * V);
     p.chains = (int)((long long)B * p.groups);
-    const int tile = is_bf16 ? tile_tokens<bf16>(back) : tile_tokens<float>(back);
-    p.tiles = L / tile + (L % tile != 0);
+    // Few chains have many of their tiles on the chip at once: listening to sixteen, and backward tiles of 16 steps, two workgroups to a
+    // compute unit, make a long sequence's chain shorter: 1 x 65536 in bf16, forward 64 channels 77 -> 62 us, 512: 91 -> 75, 1024: 107 -> 110;
+    // backward 64: 188 -> 89, 512: 209 -> 110, 1024: 234 -> 173, 1 x 16384 x 512 67 -> 42, 1 x 3000 x 512 with the mix 20 -> 22.
+    p.farther = p.chains <= (back ? 8 : 6);
+    auto tiles = [&] {
+        const int tile = is_bf16 ? tile_tokens<bf16>(back, p.farther) : tile_tokens<float>(back, p.farther);
+        p.tiles = L / tile + (L % tile != 0);
+    };
+    tiles();
+    if (p.farther && p.tiles <= (back ? 8 : 2) * kWaves) p.farther = false, tiles();
     p.how = L <= 16 ? kFew : L <= 2 * kWaves * kWalkSteps || p.chains >= 4 * device_cu_count() ? kWalk : kTiles;
-    // Few chains have many of their tiles on the chip at once, and listening to sixteen of them makes a step of the chain longer: 1 x 65536
-    // channels in bf16, forward 64: 77 -> 62 us, 512: 92 -> 76, 1024: 107 -> 110; backward 64: 188 -> 144, 1024: 234 -> 198, 2048: 316 -> 356.
-    p.farther = p.tiles > 2 * kWaves && p.chains <= (back ? 8 : 6);
     if (p.how == kTiles) p.bytes = 256 + (size_t)p.tiles * p.chains * (64 * V) * 12;
     return p;
 }

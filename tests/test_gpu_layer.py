@@ -471,6 +471,14 @@ def test_gated_few_chains(layer, B, L, D, dt):
         assert torch.equal(all_, one.repeat(12, *[1] * (one.dim() - 1)))
 
 
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("gate,mix", [("value", False), ("logit", True)])
+@pytest.mark.parametrize("B,L,D", [(1, 8300, 33), (1, 8193, 256), (1, 10000, 1024), (2, 8200, 514)])
+def test_gated_backward_few_chains(layer, B, L, D, gate, mix, dt):
+    """Both sides of the lengths and channels from which the backward's tiles are longer."""
+    test_gated_backward(layer, B, L, D, gate, mix, dt)
+
+
 @pytest.mark.parametrize("L", [40, 3000])
 def test_gated_special_values(layer, L):
     """NaN stays in its channel and sequence and reaches no earlier token; gates above one that overflow a span's product."""
