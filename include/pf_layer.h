@@ -26,6 +26,8 @@
 extern "C" {
 #endif
 
+/* Of every call here: a size that needs more workgroups than one launch holds (2^32 threads) is PF_ERR_UNSUPPORTED. */
+
 /*
  * Root-mean-square norm of rows, with the residual's addition before it and an output in 8 bits.
  *

@@ -24,6 +24,7 @@
 #include "pf_layer_internal.h"
 
 #include <algorithm>
+#include <climits>
 #include <type_traits>
 
 namespace pf {
@@ -502,8 +503,8 @@ Plan plan(int B, int L, int D, bool is_bf16, bool back)
 {
     const int V = is_bf16 ? 2 : 1;
     Plan p = {};
-    p.groups = (D + 64 * V - 1) / (64 * V);
-    p.chains = (int)((long long)B * p.groups);
+    p.groups = (int)((D + 64LL * V - 1) / (64 * V));
+    p.chains = (int)std::min((long long)B * p.groups, (long long)INT_MAX);      // (launch refuses as many)
     // Few chains have many of their tiles on the chip at once: listening to sixteen, and backward tiles of 16 steps, two workgroups to a
     // compute unit, make a long sequence's chain shorter: 1 x 65536 in bf16, forward 64 channels 77 -> 62 us, 512: 91 -> 75, 1024: 107 -> 110;
     // backward 64: 188 -> 89, 512: 209 -> 110, 1024: 234 -> 173, 1 x 16384 x 512 67 -> 42, 1 x 3000 x 512 with the mix 20 -> 22.
@@ -522,6 +523,8 @@ Plan plan(int B, int L, int D, bool is_bf16, bool back)
 template <bool BACK> hipError_t launch(const Gated &a, bool is_bf16, bool aligned, hipStream_t stream)
 {
     const Plan p = plan(a.B, a.L, a.D, is_bf16, BACK);
+    const double chains = (double)a.B * p.groups;
+    if (!launch_holds(p.how == kTiles ? chains * p.tiles : chains, p.how == kFew ? 64 : 64 * kWaves)) return hipErrorInvalidConfiguration;
     auto with_mix = [&](auto one, auto vec, auto mix) {
         using T = decltype(one);
         constexpr int V = sizeof(T) == 2 ? 2 : 1;

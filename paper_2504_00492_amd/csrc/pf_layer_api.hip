@@ -12,7 +12,10 @@ template <typename... P> bool elements_aligned(pf_dtype dt, P... p)
     return ((reinterpret_cast<uintptr_t>(p) % (dt == PF_F32 ? 4 : 2) == 0) && ...);
 }
 inline bool known(pf_dtype dt) { return dt == PF_F32 || dt == PF_BF16; }
-inline pf_status launched(hipError_t e) { return e == hipSuccess ? PF_OK : PF_ERR_LAUNCH; }
+inline pf_status launched(hipError_t e)
+{
+    return e == hipSuccess ? PF_OK : e == hipErrorInvalidConfiguration ? PF_ERR_UNSUPPORTED : PF_ERR_LAUNCH;
+}
 inline hipStream_t on(pf_stream s) { return static_cast<hipStream_t>(s); }
 
 }  // namespace

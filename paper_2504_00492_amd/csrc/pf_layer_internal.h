@@ -5,6 +5,10 @@
 
 namespace pf {
 
+// A launch holds fewer than 2^32 threads; a launcher that would need more returns hipErrorInvalidConfiguration before it launches anything.
+inline bool launch_holds(double groups, int threads) { return groups * threads < 4294967296.0; }
+
+
 // ---- root-mean-square norm (pf_norm.hip)
 constexpr int kNormWidest = 16384;
 struct NormFwd {

@@ -534,13 +534,23 @@ hipError_t launch_matmul(const Matmul &whole, bool bf16_out, hipStream_t stream)
             hipLaunchKernelGGL(matmul_join_kernel<TO>, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, stream, a, p.splits);
         }
     };
-    for (int left = whole.N; left > 0 && status == hipSuccess;) {
-        Plan p = plan_of(a.M, left, a.K, !bf16_out);
+    Plan plans[2];      // (a plan that leaves columns leaves fewer than a tile of 256)
+    int parts = 0;
+    for (int left = whole.N; left > 0; ++parts) {
+        Plan &p = plans[parts];
+        p = plan_of(a.M, left, a.K, !bf16_out);
         if (a.lda > (1 << 23) || a.ldb > (1 << 23)) p = {-1, 1, left};      // (a tile's rows are reached by 32 bits)
+        left -= p.cols;
+        const double m = a.M, n = p.cols;
+        const int rows = p.tile == 0 && !bf16_out ? 128 : p.tile < 0 ? 16 : kTileRows[p.tile], cols = p.tile < 0 ? 16 : kTileCols[p.tile];
+        if (p.tile < 0 ? !launch_holds(n / 16 + 1, 512) || m / 64 + 1 > 65535
+                       : !launch_holds((m / rows + 1) * (n / cols + 1) * p.splits, p.tile == 0 ? 512 : 256 * kTileGroups[p.tile])) return hipErrorInvalidConfiguration;
+    }
+    for (int part = 0; part < parts && status == hipSuccess; ++part) {
+        const Plan &p = plans[part];
         a.N = p.cols;
         if (bf16_out) launch((bf16)0.f, p);
         else launch(0.f, p);
-        left -= p.cols;
         a.B = static_cast<const uint8_t *>(a.B) + p.cols * a.ldb;
         a.sb += a.b_rows == 1 ? p.cols : p.cols / 128;      // (what is left begins at a multiple of 256)
         a.C = static_cast<uint8_t *>(a.C) + (size_t)p.cols * (bf16_out ? 2 : 4);

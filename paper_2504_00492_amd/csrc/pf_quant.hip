@@ -131,7 +131,7 @@ hipError_t launch_quant(const Quant &a, bool is_bf16, hipStream_t stream)
 {
     const int col_tiles = a.K / 128 + (a.K % 128 != 0);
     const long long tiles = ((a.M + 127LL) / 128) * col_tiles;
-    if (tiles * 256 >= (1LL << 32)) return hipErrorInvalidValue;      // (2^37 values)
+    if (!launch_holds((double)tiles, 256)) return hipErrorInvalidConfiguration;      // (2^37 values)
     auto launch = [&](auto one, auto vec) {
         auto with = [&](auto square, auto plain, auto turned) {
             hipLaunchKernelGGL((quant_kernel<decltype(one), vec.value, square.value, plain.value, turned.value>),

@@ -525,6 +525,66 @@ def test_gated_states(layer):
     assert torch.equal(keep, hL) and torch.equal(y, Y)
 
 
+# ---- more values than 32 bits count: the last rows, on zeros before them, are those of a call of their own
+
+def tail(rows, *shape, seed, dt=BF):
+    t = torch.zeros(rows, *shape, dtype=dt, device="cuda")
+    t[-300:] = rnd(seed, 300, *shape, dt=dt).cuda()
+    return t
+
+
+def test_norm_past_32_bits(layer):
+    M, D = 2 ** 31 // 4096 + 301, 4096
+    x, w, dy = tail(M, D, seed=1), rnd(2, D, dt=BF).cuda(), tail(M, D, seed=3)
+    for one, all_ in zip(layer.norm_fwd(x[-300:], w, eps=EPS, fp8=True)[1:3], layer.norm_fwd(x, w, eps=EPS, fp8=True)[1:3]):
+        assert torch.equal(one.view(torch.uint8), all_[-300:].view(torch.uint8))
+    dx, dw = layer.norm_bwd(x, dy, w, eps=EPS)
+    one, dw1 = layer.norm_bwd(x[-300:], dy[-300:], w, eps=EPS)
+    assert torch.equal(dx[-300:], one)
+    assert (dw - dw1).abs().max() < 1e-5 * dw1.abs().max() + 300 * U * (dy[-300:].float() * x[-300:].float()).abs().sum(0).max()
+
+
+@pytest.mark.parametrize("rows", [1, 128])
+def test_quantiser_past_32_bits(layer, rows):
+    M, K = 2 ** 31 // 4096 + 320, 4096      # (a multiple of 128 and 64 more)
+    x = tail(M, K, seed=1)
+    Q, s, QT, sT = layer.quant_fp8(x, rows=rows, transposed=True)
+    part = M // 128 * 128 - 128
+    q1, s1, qt1, st1 = layer.quant_fp8(x[part:], rows=rows, transposed=True)
+    bits = lambda t: t.view(torch.uint8)  # noqa: E731
+    assert torch.equal(bits(Q[part:]), bits(q1)) and torch.equal(bits(QT[:, part:]), bits(qt1[:, :M - part]))
+    assert torch.equal(s[:, part // rows:], s1) and torch.equal(sT[part // 128:], st1)
+
+
+@pytest.mark.parametrize("M,N,K", [(2 ** 31 // 4096 + 333, 64, 4096), (64, 2 ** 31 // 4096 + 333, 4096), (2 ** 31 // 4096 + 333, 4160, 128)])
+def test_matmul_past_32_bits(layer, M, N, K):
+    A = torch.zeros(M, K, dtype=torch.float8_e4m3fn, device="cuda")
+    B = torch.zeros(N, K, dtype=torch.float8_e4m3fn, device="cuda")
+    A[-40:], B[-40:] = rnd(1, 40, K).cuda().to(A.dtype), rnd(2, 40, K).cuda().to(B.dtype)
+    sa, sb = torch.ones(K // 128, M, device="cuda"), torch.ones(K // 128, N, device="cuda")
+    for dt in (F32, BF):
+        C = layer.matmul_fp8(A, sa, B, sb, b_rows=1, out_dtype=dt)
+        a, b = A[-40:].double().cpu(), B[-40:].double().cpu()
+        ref = a @ b.t()
+        near(C[-40:, -40:], ref, (HALF[dt] + 2 ** -10 * (dt == BF) + K * U) * (a.abs() @ b.abs().t()))
+        assert (C[:-40, -40:][:4].float() == 0).all() and (C[-40:, :4].float() == 0).all()
+
+
+@pytest.mark.parametrize("B,L,D", [(1, 2 ** 31 // 2048 + 301, 2048), (2 ** 31 // 4096 + 301, 1, 4096), (2 ** 31 // 32768 + 301, 32, 1024)])
+def test_gated_past_32_bits(layer, B, L, D):
+    x, dy = (tail(B * L, D, seed=s).view(B, L, D) for s in (1, 2))
+    g = torch.full_like(x, -0.5)
+    Y, hL = layer.gated_fwd(x, g)
+    dX, dG, dh0 = layer.gated_bwd(None, g, Y, dy)
+    cut = (lambda t: t[:, -300:].contiguous()) if B == 1 else (lambda t: t[-9:].contiguous())
+    ref, tol = gated_ref(cut(x).cpu(), cut(g).cpu(), None, "log", False)
+    near(cut(Y), ref, tol + HALF[BF] * ref.abs())
+    near(hL[-1], ref[-1, -1], tol[-1, -1])
+    zero = torch.zeros(ref.shape[0], D)
+    for out, (r, t) in zip((dX, dG), gated_grads(cut(x).cpu(), cut(g).cpu(), zero, cut(Y).cpu(), cut(dy).cpu(), zero, "log", False)):
+        near(cut(out), r, t + HALF[BF] * r.abs())
+
+
 # ---- as a user calls them
 
 def _calls(layer):

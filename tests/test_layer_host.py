@@ -103,6 +103,18 @@ def test_refusals(layer, call, wrong, status):
     assert call(layer, **wrong) == status
 
 
+@pytest.mark.parametrize("call,sizes", [
+    (_quant, dict(M=(1 << 31) - 1, K=640, ldx=640, ldq=640, ldqt=1 << 31)),
+    (_matmul, dict(M=1, N=(1 << 31) - 1, ldc=1 << 31)), (_matmul, dict(M=(1 << 31) - 1, N=272, ldc=272)),
+    (_matmul, dict(M=(1 << 31) - 1, N=272, ldc=272, dt=F32)), (_matmul, dict(M=1 << 23, N=2, ldb=1 << 24)),
+    (_gated_fwd, dict(B=1 << 26, L=1, D=1)), (_gated_fwd, dict(B=1 << 23, L=20, D=1)), (_gated_fwd, dict(B=(1 << 31) - 1, L=0, D=1 << 20)),
+    (_gated_bwd, dict(B=2, L=1 << 30, D=1)), (_gated_bwd, dict(B=1 << 20, L=17, D=1 << 20))])
+def test_more_than_a_launch_holds(layer, call, sizes):
+    """Refused on the host, before any work."""
+    assert call(layer, **sizes) == UNSUPPORTED
+
+
+
 def test_workspace_too_small(layer):
     need = layer.pf_gated_workspace_bytes(1, 65536, 4096, BF16)
     if need:
