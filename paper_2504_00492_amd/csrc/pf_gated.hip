@@ -15,7 +15,7 @@
 // out before its own, whose workgroups are on the chip already and wait for nothing later, so every wait ends.  What a tile makes of
 // the values that come in depends on the tiles between them in order, whichever were told, so the bits do not depend on timing.
 //
-// Bound by HBM: 1 x 65536 x 4096 forward in bf16 321 us, 5.0 TB/s (a plain copy: 5.1); 1 x 65536 x 2048 in fp32 5.5 TB/s; backward with
+// Bound by HBM: 1 x 65536 x 4096 forward in bf16 312 us, 5.2 TB/s (a plain copy: 5.1); 1 x 65536 x 2048 in fp32 5.5 TB/s; backward with
 // the mix 2 x 8192 x 4096 183 us, 4.4 TB/s, where the tiles are not long enough for what a tile waits to be hidden.  A long sequence of few
 // channels is bound by the chain, 0.18 us a tile: 1 x 65536 x 64 62 us.  Tried and left: two channels more to a lane (321 -> 375 us), workgroups
 // that draw tile after tile and read ahead (475: what they hold in registers makes tiles short), 16 tiles listened to here too (twice the words
@@ -33,12 +33,13 @@ namespace {
 
 constexpr int kWaves = 8, kWalkSteps = 16;
 // Steps of a wavefront's span of a tile, as its registers allow: forward (two arrays) two workgroups to a compute unit, of tiles that are
-// long, so that there is less to tell and to wait for (1 x 65536 x 4096, bf16: 16 steps 351 us, 24 320); backward (up to four
+// long, so that there is less to tell and to wait for (1 x 65536 x 4096, bf16: 16 steps 351 us, 24 320, 28 311; 32 1 to 4 % more than 28); backward (up to four
 // arrays) three of short ones (2 x 8192 x 4096: two of 16 steps 188 us, three of 9 183; 16 x 2048 x 4096 316 and 314).
-template <typename T, bool BACK, bool FARTHER = false> constexpr int kTileSteps = BACK ? (FARTHER ? 16 : 9) : sizeof(T) == 2 ? 24 : 32;
-template <typename T> inline int tile_tokens(bool back, bool farther)
+template <typename T, bool BACK, bool MIX, bool FARTHER>
+constexpr int kTileSteps = BACK ? (FARTHER ? 16 : 9) : sizeof(T) == 4 ? 32 : FARTHER ? 24 : MIX ? 20 : 28;
+template <typename T, bool BACK, bool MIX> constexpr int tile_tokens(bool farther)
 {
-    return kWaves * (!back ? kTileSteps<T, false> : farther ? kTileSteps<T, true, true> : kTileSteps<T, true>);
+    return kWaves * (farther ? kTileSteps<T, BACK, MIX, true> : kTileSteps<T, BACK, MIX, false>);
 }
 
 // the decay a, 1 - a, and d a / d g of a gate's value
@@ -186,17 +187,18 @@ template <typename T, int V, bool VEC, bool BACK> struct Chain {
     }
 };
 
-template <typename K, int N, bool BACK = K::BACK> struct Span;
+template <typename K, int N, bool KEPT, bool BACK = K::BACK> struct Span;
 
-// Forward: N steps in registers, as they lie in memory; the gates are kept between the two times they are needed, but with
-// the mix they are formed again (half the registers).
-template <typename K, int N> struct Span<K, N, false> {
+// Forward: N steps in registers.  Each is needed twice.  KEPT, with the mix, whose gates cost most: a and b stay in registers once they are
+// formed (fp32: in the place of g and x; bf16: twice that, so fewer steps).  2 x 8192 x 4096 in bf16, 24 steps formed twice 111 us, 20 kept
+// 99; 64 x 512 x 2048 107 and 90; 3 x 4099 x 1001 in fp32 45.5 and 43.0.  Without the mix they are formed twice.
+template <typename K, int N, bool KEPT> struct Span<K, N, KEPT, false> {
     using T = typename K::T;
     static constexpr int V = K::V, FORM = K::FORM;
     static constexpr bool VEC = K::VEC, MIX = K::MIX;
     using C = Chain<T, V, VEC, false>;
     Raw<T, V> x[N], g[N];
-    
+    float a[KEPT ? N : 1][V], b[KEPT ? N : 1][V];
     __device__ __forceinline__ void read(const C &c, int s0)
     {
 #pragma unroll
@@ -216,9 +218,10 @@ template <typename K, int N> struct Span<K, N, false> {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const Gate k = gate_of<FORM, MIX>(value(g[i], v));
-                const float in = value(x[i], v), now = s0 + i < c.a.L ? k.a : 1.f;      // (behind the end x is zero)
+                const float in = MIX ? k.rest * value(x[i], v) : value(x[i], v), now = s0 + i < c.a.L ? k.a : 1.f;      // (behind the end x is zero)
+                if constexpr (KEPT) a[i][v] = k.a, b[i][v] = in;
                 A[v] *= now;
-                H[v] = fmaf(now, H[v], MIX ? k.rest * in : in);
+                H[v] = fmaf(now, H[v], in);
                 if (v == V - 1 && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);      // (all gates side by side would not fit the registers)
             }
     }
@@ -227,12 +230,15 @@ template <typename K, int N> struct Span<K, N, false> {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             if (s0 + i >= c.a.L) break;
-            afresh(g[i]);
+            if constexpr (!KEPT) afresh(g[i]);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const Gate k = gate_of<FORM, MIX>(value(g[i], j));
-                const float in = value(x[i], j);
-                v[j] = fmaf(k.a, v[j], MIX ? k.rest * in : in);
+                if constexpr (KEPT) {
+                    v[j] = fmaf(a[i][j], v[j], b[i][j]);
+                } else {
+                    const Gate k = gate_of<FORM, MIX>(value(g[i], j));
+                    v[j] = fmaf(k.a, v[j], MIX ? k.rest * value(x[i], j) : value(x[i], j));
+                }
             }
             keep<T, V, VEC>(c.o0 + (long long)(s0 + i) * c.a.D + c.mine, v, c.left);
             if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
@@ -240,7 +246,7 @@ template <typename K, int N> struct Span<K, N, false> {
     }
 };
 
-template <typename K, int N> struct Span<K, N, true> {
+template <typename K, int N, bool KEPT> struct Span<K, N, KEPT, true> {
     using T = typename K::T;
     static constexpr int V = K::V, FORM = K::FORM;
     static constexpr bool VEC = K::VEC, MIX = K::MIX;
@@ -311,7 +317,7 @@ __device__ __forceinline__ void gated_walk(const Gated &a, int groups, Pair (&sp
     const Chain<T, V, VEC, K::BACK> c(a, blockIdx.x, groups, lane);
     float in[V];
     c.incoming(in);
-    Span<K, kWalkSteps> s;
+    Span<K, kWalkSteps, !K::BACK && K::MIX> s;
     for (int s0 = 0, turn = 0; s0 < a.L; s0 += kWaves * kWalkSteps, turn ^= 1) {
         const int mine = s0 + w * kWalkSteps;
         s.read(c, mine);
@@ -351,10 +357,10 @@ __device__ __forceinline__ void gated_tile(const Gated &a, int groups, int chain
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t id = __builtin_amdgcn_readfirstlane(lds.ticket);
     const int tile = __builtin_amdgcn_readfirstlane(id / chains), chain = (int)id - tile * chains;      // (unsigned division is done in the lanes)
-    constexpr int steps = kTileSteps<T, K::BACK, (PER > 1)>;
+    constexpr int steps = kTileSteps<T, K::BACK, K::MIX, (PER > 1)>;
     const int mine = (tile * kWaves + w) * steps;
     const Chain<T, V, VEC, K::BACK> c(a, chain, groups, lane);
-    Span<K, steps> s;
+    Span<K, steps, !K::BACK && K::MIX && (sizeof(T) == 4 || PER == 1)> s;
     s.read(c, mine);
     float A[V], H[V];
     s.gates(c, mine, A, H);
@@ -455,7 +461,7 @@ __device__ __forceinline__ void gated_few(const Gated &a, int groups)
     const Chain<T, V, VEC, K::BACK> c(a, blockIdx.x, groups, threadIdx.x);
     float v[V];
     c.incoming(v);
-    Span<K, 4> s;
+    Span<K, 4, false> s;
     for (int s0 = 0; s0 < a.L; s0 += 4) {
         s.read(c, s0);
         float A[V], H[V];
@@ -499,7 +505,7 @@ struct Plan {
     bool farther;
     size_t bytes;
 };
-Plan plan(int B, int L, int D, bool is_bf16, bool back)
+Plan plan(int B, int L, int D, bool is_bf16, bool back, bool mix)
 {
     const int V = is_bf16 ? 2 : 1;
     Plan p = {};
@@ -510,11 +516,12 @@ Plan plan(int B, int L, int D, bool is_bf16, bool back)
     // backward 64: 188 -> 89, 512: 209 -> 110, 1024: 234 -> 173, 1 x 16384 x 512 67 -> 42, 1 x 3000 x 512 with the mix 20 -> 22.
     p.farther = p.chains <= (back ? 8 : 6);
     auto tiles = [&] {
-        const int tile = is_bf16 ? tile_tokens<bf16>(back, p.farther) : tile_tokens<float>(back, p.farther);
+        const int tile = back ? tile_tokens<bf16, true, false>(p.farther) : !is_bf16 ? tile_tokens<float, false, false>(p.farther)
+                         : mix ? tile_tokens<bf16, false, true>(p.farther) : tile_tokens<bf16, false, false>(p.farther);
         p.tiles = L / tile + (L % tile != 0);
     };
     tiles();
-    if (p.farther && p.tiles <= (back ? 8 : 2) * kWaves) p.farther = false, tiles();
+    if (p.farther && p.tiles <= 8 * kWaves) p.farther = false, tiles();
     p.how = L <= 16 ? kFew : L <= 2 * kWaves * kWalkSteps || p.chains >= 4 * device_cu_count() ? kWalk : kTiles;
     if (p.how == kTiles) p.bytes = 256 + (size_t)p.tiles * p.chains * (64 * V) * 12;
     return p;
@@ -522,7 +529,7 @@ Plan plan(int B, int L, int D, bool is_bf16, bool back)
 
 template <bool BACK> hipError_t launch(const Gated &a, bool is_bf16, bool aligned, hipStream_t stream)
 {
-    const Plan p = plan(a.B, a.L, a.D, is_bf16, BACK);
+    const Plan p = plan(a.B, a.L, a.D, is_bf16, BACK, a.mix);
     const double chains = (double)a.B * p.groups;
     if (!launch_holds(p.how == kTiles ? chains * p.tiles : chains, p.how == kFew ? 64 : 64 * kWaves)) return hipErrorInvalidConfiguration;
     auto with_mix = [&](auto one, auto vec, auto mix) {
@@ -571,7 +578,8 @@ inline bool words(const void *p, long long batch, long long token)
 
 size_t gated_workspace_bytes(int B, int L, int D, bool is_bf16)
 {
-    const size_t n = std::max(plan(B, L, D, is_bf16, false).bytes, plan(B, L, D, is_bf16, true).bytes);
+    const size_t n = std::max({plan(B, L, D, is_bf16, false, false).bytes, plan(B, L, D, is_bf16, false, true).bytes,
+                               plan(B, L, D, is_bf16, true, false).bytes});
     return (n + 15) / 16 * 16;
 }
 

@@ -3,7 +3,7 @@
 // m = max(max|x| over the block, 1e-30), scale = m * (1/448), value = e4m3(x * (1/m * 448)), each operation rounded in fp32.
 // A workgroup takes a tile of 128 x 128: a thread eight rows by eight columns in registers, so a row of the tile is sixteen
 // lanes, a column sixteen groups of them.  Memory sees x once, whatever is written of it.  Bound by HBM: 8192 x 4096 in bf16, transposed,
-// 26 us, 3.9 TB/s.
+// 23 us, 4.4 TB/s; 32768 x 4096 4.8, as it lies 5.1.
 #include "pf_layer_common.h"
 #include "pf_layer_internal.h"
 

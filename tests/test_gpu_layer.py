@@ -472,6 +472,14 @@ def test_gated_few_chains(layer, B, L, D, dt):
 
 
 @pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("gate,mix", [("log", False), ("logit", True)])
+@pytest.mark.parametrize("B,L,D", [(1, 12289, 256), (1, 14400, 33), (2, 17000, 131), (1, 16500, 900)])
+def test_gated_few_chains_longer(layer, B, L, D, gate, mix, dt):
+    """The lengths from which more tiles in front are listened to."""
+    test_gated(layer, B, L, D, gate, mix, dt)
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
 @pytest.mark.parametrize("gate,mix", [("value", False), ("logit", True)])
 @pytest.mark.parametrize("B,L,D", [(1, 8300, 33), (1, 8193, 256), (1, 10000, 1024), (2, 8200, 514)])
 def test_gated_backward_few_chains(layer, B, L, D, gate, mix, dt):
