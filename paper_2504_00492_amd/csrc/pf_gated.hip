@@ -366,6 +366,13 @@ __device__ __forceinline__ void gated_tile(const Gated &a, int groups, int chain
     s.gates(c, mine, A, H);
 #pragma unroll
     for (int v = 0; v < V; ++v) lds.spans[w][v][lane] = {A[v], H[v]};
+    float in[V];
+    if (tile == 0 && w == 0) {
+        // read once, and there before anything of this tile is told: what goes out of the chain may be written in its place
+        c.incoming(in);
+#pragma unroll
+        for (int v = 0; v < V; ++v) lds.outs[0][v][lane] = in[v];
+    }
     __syncthreads();
     // words of a tile of this chain lie side by side: [tile][chain][v][lane]
     const long long row = (long long)chains * (64 * V), at = (long long)tile * row + (long long)chain * (64 * V);
@@ -382,9 +389,9 @@ __device__ __forceinline__ void gated_tile(const Gated &a, int groups, int chain
 #pragma unroll
             for (int v = 0; v < V; ++v) tell(work.span + at + 64 * v + (unsigned)lane, (unsigned long long)told(H[v]) << 32 | told(A[v]));
     }
-    float in[V];
     if (tile == 0) {
-        c.incoming(in);
+#pragma unroll
+        for (int v = 0; v < V; ++v) in[v] = lds.outs[0][v][lane];
     } else {      // each wavefront listens to PER of the tiles in front
         bool has_out[PER] = {}, has_span[PER] = {};
         int from;
