@@ -136,7 +136,8 @@ pf_status pf_matmul_fp8(const void *A, long long lda, const float *sa, const voi
  *
  * L == 0: hL receives h0 (or zeros), the sequence pointers may be NULL.  B == 0: nothing is done.  L up to 2^30
  * (PF_ERR_UNSUPPORTED).
- * Where h overflows to infinity, later values may be NaN instead of infinite.
+ * Where the same recurrence over the sizes |a|, |b|, |h0| stays inside fp32, this one does too, however far products of gates leave it;
+ * where that one overflows, values may be infinite or NaN from there on.
  */
 typedef enum { PF_GATE_VALUE = 0, PF_GATE_LOG = 1, PF_GATE_LOGIT = 2 } pf_gate;
 

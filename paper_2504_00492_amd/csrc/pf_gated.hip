@@ -2,7 +2,8 @@
 // the other way: with m = a_{t+1} l_{t+1} coming in, l_t = dy_t + m and a_t l_t goes out.
 //
 // A span of steps takes what comes in, v, to A v + H: A the product of its gates, H what it makes of zero.  Spans join as
-// (A, H) then (A', H') = (A' A, A' H + H'), so they can be read side by side.  A wavefront holds 64 V channels of some
+// (A, H) then (A', H') = (A' A, A' H + H'), so they can be read side by side.  A is kept as m 2^e: with gates of 2 and then 1/2 it
+// leaves fp32 where no state does, and from then on it would be lost.  A wavefront holds 64 V channels of some
 // consecutive steps in registers, a workgroup kWaves such spans, one behind the other: a tile.  Each span's (A, H) is formed first, the
 // spans in front are put through it, and the steps run once more from what really comes in.  Memory sees every array once.
 //
@@ -69,8 +70,31 @@ template <int FORM, bool MIX> __device__ __forceinline__ Gate gate_of(float g)
     return {g < 0.f ? t : s, g < 0.f ? s : t, t * s};
 }
 
-// what a span makes of v; nothing coming in stays nothing where the product of the gates is beyond fp32
-__device__ __forceinline__ float through(float A, float H, float v) { return v == 0.f ? H : fmaf(A, v, H); }
+// A product of gates, m 2^e: while it is formed 1/2 <= |m| < 1 (or zero, infinite, NaN), when it is used 1 <= |m| < 2, so that 2^e v is
+// beyond fp32 only where the whole is.  What that costs, against a product that is one number: 1 x 65536 x 4096 in bf16 317 -> 326 us.
+struct Product {
+    float m = 0.5f;
+    int e = 1;
+    __device__ __forceinline__ void times(float a)
+    {
+        const float n = m * a;
+        m = __builtin_amdgcn_frexp_mantf(n);
+        e += __builtin_amdgcn_frexp_expf(n);
+    }
+    __device__ __forceinline__ void ready() { m += m, --e; }
+};
+// what a span makes of v
+__device__ __forceinline__ float through(float m, int e, float H, float v) { return fmaf(m, __builtin_ldexpf(v, e), H); }
+
+// the powers of V neighbouring channels in one word, which is never clear (below)
+constexpr int kPowerZero = 1 << 14;
+template <int V> __device__ __forceinline__ uint32_t powers(const Product (&A)[V])
+{
+    const uint32_t w = A[0].e + kPowerZero;      // (32 steps: 4800 at most)
+    if constexpr (V == 2) return w | (uint32_t)(A[1].e + kPowerZero) << 16;
+    return w;
+}
+__device__ __forceinline__ int power(uint32_t w, int v) { return (int)(w >> (16 * v) & 0xffff) - kPowerZero; }
 
 // V neighbouring channels of one token
 template <typename T, int V> struct Raw { uint32_t w[(sizeof(T) * V + 3) / 4]; };
@@ -80,6 +104,9 @@ template <typename T, int V> __device__ __forceinline__ void afresh(Raw<T, V> &r
 #pragma unroll
     for (auto &w : r.w) asm volatile("" : "+v"(w));
 }
+// formed step by step: what all steps add, side by side until it is summed, would not fit the registers
+__device__ __forceinline__ void here(int &e) { asm volatile("" : "+v"(e)); }
+__device__ __forceinline__ void here(float &f) { asm volatile("" : "+v"(f)); }
 template <typename T, int V, bool VEC> __device__ __forceinline__ Raw<T, V> fetch(const T *p, int left)
 {
     Raw<T, V> r = {};
@@ -126,10 +153,12 @@ __device__ __forceinline__ uint32_t told(float f)
 template <typename W> __device__ __forceinline__ void tell(W *p, W w) { __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 template <typename W> __device__ __forceinline__ W hear(const W *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
+template <int V> using OutWord = std::conditional_t<V == 2, unsigned long long, uint32_t>;
 struct Work {
     uint32_t *next;          // the counter that hands out tiles
-    unsigned long long *span; // [tile][channel] A, H
-    uint32_t *out;           // [tile][channel] what goes out
+    unsigned long long *span; // [tile][channel] m, H
+    uint32_t *power;         // [tile][lane] e of its channels
+    void *out;               // [tile][lane] what goes out of its channels, one word
 };
 
 // steps of a chain in the order of the recurrence: step s is token s, or of the backward token L - 1 - s
@@ -146,7 +175,7 @@ template <typename T, int V, bool VEC, bool BACK> struct Chain {
     T *o0, *o1;
     const float *in;
     float *out;
-    long long state;
+    long long state;    // (of the first channel)
     int left;           // channels from this lane's first on
     unsigned mine;      // this lane's first
     __device__ __forceinline__ Chain(const Gated &a_, int chain, int groups, int lane) : a(a_)
@@ -157,7 +186,7 @@ template <typename T, int V, bool VEC, bool BACK> struct Chain {
         mine = lane * V;
         left = a.D - c - (int)mine;
         const long long at = b * a.L * a.D + c;
-        state = b * a.D + c + mine;
+        state = b * a.D + c;
         x = static_cast<const T *>(a.X) + (a.X ? b * a.xb + c : 0);
         g = static_cast<const T *>(a.G) + b * a.gb + c;
         if constexpr (BACK) {
@@ -176,14 +205,14 @@ template <typename T, int V, bool VEC, bool BACK> struct Chain {
     __device__ __forceinline__ void incoming(float (&v)[V]) const
     {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = in && i < left ? in[state + i] : 0.f;
+        for (int i = 0; i < V; ++i) v[i] = in && i < left ? in[state + mine + i] : 0.f;
     }
     __device__ __forceinline__ void outgoing(const float (&v)[V]) const
     {
         if (out)
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                if (i < left) out[state + i] = v[i];
+                if (i < left) out[state + mine + i] = v[i];
     }
 };
 
@@ -209,10 +238,10 @@ template <typename K, int N, bool KEPT> struct Span<K, N, KEPT, false> {
             x[i] = fetch<T, V, VEC>(c.x + t * c.a.xt + c.mine, left);
         }
     }
-    __device__ __forceinline__ void gates(const C &c, int s0, float (&A)[V], float (&H)[V])
+    __device__ __forceinline__ void gates(const C &c, int s0, Product (&A)[V], float (&H)[V])
     {
 #pragma unroll
-        for (int v = 0; v < V; ++v) A[v] = 1.f, H[v] = 0.f;
+        for (int v = 0; v < V; ++v) A[v] = {}, H[v] = 0.f;
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
@@ -220,10 +249,13 @@ template <typename K, int N, bool KEPT> struct Span<K, N, KEPT, false> {
                 const Gate k = gate_of<FORM, MIX>(value(g[i], v));
                 const float in = MIX ? k.rest * value(x[i], v) : value(x[i], v), now = s0 + i < c.a.L ? k.a : 1.f;      // (behind the end x is zero)
                 if constexpr (KEPT) a[i][v] = k.a, b[i][v] = in;
-                A[v] *= now;
+                A[v].times(now);
                 H[v] = fmaf(now, H[v], in);
+                here(A[v].e);
                 if (v == V - 1 && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);      // (all gates side by side would not fit the registers)
             }
+#pragma unroll
+        for (int v = 0; v < V; ++v) A[v].ready();
     }
     __device__ __forceinline__ void run(const C &c, int s0, float (&v)[V])
     {
@@ -265,19 +297,23 @@ template <typename K, int N, bool KEPT> struct Span<K, N, KEPT, true> {
             if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);      // (the addresses of all rows would not fit the scalar registers)
         }
     }
-    __device__ __forceinline__ void gates(const C &c, int s0, float (&A)[V], float (&H)[V])
+    __device__ __forceinline__ void gates(const C &c, int s0, Product (&A)[V], float (&H)[V])
     {
 #pragma unroll
-        for (int v = 0; v < V; ++v) A[v] = 1.f, H[v] = 0.f;
+        for (int v = 0; v < V; ++v) A[v] = {}, H[v] = 0.f;
 #pragma unroll
         for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const float a = s0 + i < c.a.L ? gate_of<FORM, false>(value(g[i], v)).a : 1.f;
-                A[v] *= a;
+                A[v].times(a);
                 H[v] = a * (value(dy[i], v) + H[v]);
+                here(A[v].e);
+                here(H[v]);
                 if (v == V - 1 && i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
             }
+#pragma unroll
+        for (int v = 0; v < V; ++v) A[v].ready();
     }
     __device__ __forceinline__ void run(const C &c, int s0, float (&v)[V])
     {
@@ -286,12 +322,13 @@ template <typename K, int N, bool KEPT> struct Span<K, N, KEPT, true> {
             const long long t = (long long)c.a.L - 1 - s0 - i;
             if (t < 0) break;
             afresh(g[i]);
+            afresh(dy[i]);
             float dx[V], dg[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const Gate k = gate_of<FORM, MIX>(value(g[i], j));
                 const float l = value(dy[i], j) + v[j];
-                float h = t > 0 ? value(y[i], j) : c.a.h0 && j < c.left ? c.a.h0[c.state + j] : 0.f;
+                float h = t > 0 ? value(y[i], j) : c.a.h0 && j < c.left ? c.a.h0[c.state + c.mine + j] : 0.f;
                 if (MIX) h -= value(x[MIX ? i : 0], j);
                 dx[j] = MIX ? k.rest * l : l;
                 dg[j] = l * h * k.slope;
@@ -304,11 +341,15 @@ template <typename K, int N, bool KEPT> struct Span<K, N, KEPT, true> {
     }
 };
 
-struct Pair { float A, H; };
+struct Pair { float m, H; };
+template <int V> struct WalkLds {
+    Pair spans[2][kWaves][V][64];
+    uint32_t powers[2][kWaves][64];
+};
 
 // A workgroup for each chain, from tile to tile.
 template <typename K>
-__device__ __forceinline__ void gated_walk(const Gated &a, int groups, Pair (&spans)[2][kWaves][K::V][64])
+__device__ __forceinline__ void gated_walk(const Gated &a, int groups, WalkLds<K::V> &lds)
 {
     using T = typename K::T;
     constexpr int V = K::V;
@@ -321,19 +362,22 @@ __device__ __forceinline__ void gated_walk(const Gated &a, int groups, Pair (&sp
     for (int s0 = 0, turn = 0; s0 < a.L; s0 += kWaves * kWalkSteps, turn ^= 1) {
         const int mine = s0 + w * kWalkSteps;
         s.read(c, mine);
-        float A[V], H[V];
+        Product A[V];
+        float H[V];
         s.gates(c, mine, A, H);
 #pragma unroll
-        for (int v = 0; v < V; ++v) spans[turn][w][v][lane] = {A[v], H[v]};
+        for (int v = 0; v < V; ++v) lds.spans[turn][w][v][lane] = {A[v].m, H[v]};
+        lds.powers[turn][w][lane] = powers(A);
         __syncthreads();
         float now[V];
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < kWaves; ++i) {
+            const uint32_t e = lds.powers[turn][i][lane];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 if (i == w) now[v] = in[v];
-                const Pair p = spans[turn][i][v][lane];
-                in[v] = through(p.A, p.H, in[v]);
+                const Pair p = lds.spans[turn][i][v][lane];
+                in[v] = through(p.m, power(e, v), p.H, in[v]);
             }
         }
         s.run(c, mine, now);
@@ -344,6 +388,7 @@ __device__ __forceinline__ void gated_walk(const Gated &a, int groups, Pair (&sp
 // A workgroup for each tile.
 template <int V, int PER> struct TileLds {
     Pair spans[kWaves][V][64], behind[kWaves * PER][V][64];
+    uint32_t powers[kWaves][64], behind_powers[kWaves * PER][64];
     float outs[kWaves * PER][V][64];
     int heard[kWaves * PER];      // of a tile in front: 1 its (A, H), 2 what goes out of it
     uint32_t ticket;
@@ -362,10 +407,12 @@ __device__ __forceinline__ void gated_tile(const Gated &a, int groups, int chain
     const Chain<T, V, VEC, K::BACK> c(a, chain, groups, lane);
     Span<K, steps, !K::BACK && K::MIX && (sizeof(T) == 4 || PER == 1)> s;
     s.read(c, mine);
-    float A[V], H[V];
+    Product A[V];
+    float H[V];
     s.gates(c, mine, A, H);
 #pragma unroll
-    for (int v = 0; v < V; ++v) lds.spans[w][v][lane] = {A[v], H[v]};
+    for (int v = 0; v < V; ++v) lds.spans[w][v][lane] = {A[v].m, H[v]};
+    lds.powers[w][lane] = powers(A);
     float in[V];
     if (tile == 0 && w == 0) {
         // read once, and there before anything of this tile is told: what goes out of the chain may be written in its place
@@ -376,18 +423,27 @@ __device__ __forceinline__ void gated_tile(const Gated &a, int groups, int chain
     __syncthreads();
     // words of a tile of this chain lie side by side: [tile][chain][v][lane]
     const long long row = (long long)chains * (64 * V), at = (long long)tile * row + (long long)chain * (64 * V);
+    const long long power_row = (long long)chains * 64, power_at = (long long)tile * power_row + (long long)chain * 64;
     if (w == 0 && tile < tiles - 1) {
-#pragma unroll
-        for (int i = 1; i < kWaves; ++i)
+#pragma unroll 1
+        for (int i = 1; i < kWaves; ++i) {
+            const uint32_t e = lds.powers[i][lane];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const Pair p = lds.spans[i][v][lane];
-                A[v] *= p.A;
-                H[v] = fmaf(p.A, H[v], p.H);
+                H[v] = through(p.m, power(e, v), p.H, H[v]);
+                A[v].times(p.m);
+                A[v].e += power(e, v);
+                A[v].ready();
             }
-        if (tile > 0)
+        }
 #pragma unroll
-            for (int v = 0; v < V; ++v) tell(work.span + at + 64 * v + (unsigned)lane, (unsigned long long)told(H[v]) << 32 | told(A[v]));
+        for (int v = 0; v < V; ++v) A[v].e = min(max(A[v].e, -400), 400);      // (a power of 400 takes every state out of fp32)
+        if (tile > 0) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) tell(work.span + at + 64 * v + (unsigned)lane, (unsigned long long)told(H[v]) << 32 | told(A[v].m));
+            tell(work.power + power_at + (unsigned)lane, powers(A));
+        }
     }
     if (tile == 0) {
 #pragma unroll
@@ -408,17 +464,15 @@ __device__ __forceinline__ void gated_tile(const Gated &a, int groups, int chain
                         ready = ready && (uint32_t)p != kClear;
                         lds.behind[k][v][lane] = {__uint_as_float((uint32_t)p), __uint_as_float((uint32_t)(p >> 32))};
                     }
-                    has_span[q] = __all(ready);
+                    const uint32_t e = hear(work.power + power_at - (k + 1) * power_row + (unsigned)lane);
+                    lds.behind_powers[k][lane] = e;
+                    has_span[q] = __all(ready && e != kClear);
                 }
                 if (!has_out[q] && k < tile) {
-                    bool ready = true;
+                    const OutWord<V> o = hear(static_cast<const OutWord<V> *>(work.out) + (power_at - (k + 1) * power_row) + (unsigned)lane);
 #pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        const uint32_t o = hear(work.out + there + 64 * v + (unsigned)lane);
-                        ready = ready && o != kClear;
-                        lds.outs[k][v][lane] = __uint_as_float(o);
-                    }
-                    has_out[q] = __all(ready);
+                    for (int v = 0; v < V; ++v) lds.outs[k][v][lane] = __uint_as_float((uint32_t)(v ? o >> 16 >> 16 : o));
+                    has_out[q] = __all((uint32_t)o != kClear);
                 }
                 if (lane == 0) lds.heard[k] = (has_span[q] ? 1 : 0) | (has_out[q] ? 2 : 0);
             }
@@ -438,17 +492,24 @@ __device__ __forceinline__ void gated_tile(const Gated &a, int groups, int chain
 #pragma unroll
         for (int v = 0; v < V; ++v) in[v] = lds.outs[from][v][lane];
 #pragma unroll 1
-        for (int k = from - 1; k >= 0; --k)
+        for (int k = from - 1; k >= 0; --k) {
+            const uint32_t e = lds.behind_powers[k][lane];
 #pragma unroll
-            for (int v = 0; v < V; ++v) in[v] = through(lds.behind[k][v][lane].A, lds.behind[k][v][lane].H, in[v]);
+            for (int v = 0; v < V; ++v) in[v] = through(lds.behind[k][v][lane].m, power(e, v), lds.behind[k][v][lane].H, in[v]);
+        }
     }
-    if (w == 0 && tile < tiles - 1)
+    if (w == 0 && tile < tiles - 1) {
+        OutWord<V> o = 0;
 #pragma unroll
-        for (int v = 0; v < V; ++v) tell(work.out + at + 64 * v + (unsigned)lane, told(through(A[v], H[v], in[v])));
+        for (int v = 0; v < V; ++v) o |= (OutWord<V>)told(through(A[v].m, A[v].e, H[v], in[v])) << (32 * v);
+        tell(static_cast<OutWord<V> *>(work.out) + power_at + (unsigned)lane, o);
+    }
 #pragma unroll 1
-    for (int i = 0; i < w; ++i)
+    for (int i = 0; i < w; ++i) {
+        const uint32_t e = lds.powers[i][lane];
 #pragma unroll
-        for (int v = 0; v < V; ++v) in[v] = through(lds.spans[i][v][lane].A, lds.spans[i][v][lane].H, in[v]);
+        for (int v = 0; v < V; ++v) in[v] = through(lds.spans[i][v][lane].m, power(e, v), lds.spans[i][v][lane].H, in[v]);
+    }
     s.run(c, mine, in);
     if (tile == tiles - 1 && w == kWaves - 1) c.outgoing(in);
 }
@@ -471,8 +532,6 @@ __device__ __forceinline__ void gated_few(const Gated &a, int groups)
     Span<K, 4, false> s;
     for (int s0 = 0; s0 < a.L; s0 += 4) {
         s.read(c, s0);
-        float A[V], H[V];
-        s.gates(c, s0, A, H);
         s.run(c, s0, v);
     }
     c.outgoing(v);
@@ -486,10 +545,10 @@ template <typename T, int V, bool VEC, bool BACK, bool MIX, typename F> __device
     else f(Kind<T, V, VEC, BACK, MIX, 2>{});
 }
 template <typename T, int V, bool VEC, bool BACK, bool MIX>
-__global__ __launch_bounds__(64 * kWaves) void gated_walk_kernel(Gated a, int groups)
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(4))) void gated_walk_kernel(Gated a, int groups)
 {
-    __shared__ Pair spans[2][kWaves][V][64];
-    by_form<T, V, VEC, BACK, MIX>(a.gate, [&](auto k) { gated_walk<decltype(k)>(a, groups, spans); });
+    __shared__ WalkLds<V> lds;
+    by_form<T, V, VEC, BACK, MIX>(a.gate, [&](auto k) { gated_walk<decltype(k)>(a, groups, lds); });
 }
 // (so many wavefronts to a SIMD; where channels lie at odd places their registers allow three)
 template <typename T, int V, bool VEC, bool BACK, bool MIX, int PER>
@@ -530,7 +589,7 @@ Plan plan(int B, int L, int D, bool is_bf16, bool back, bool mix)
     tiles();
     if (p.farther && p.tiles <= 8 * kWaves) p.farther = false, tiles();
     p.how = L <= 16 ? kFew : L <= 2 * kWaves * kWalkSteps || p.chains >= 4 * device_cu_count() ? kWalk : kTiles;
-    if (p.how == kTiles) p.bytes = 256 + (size_t)p.tiles * p.chains * (64 * V) * 12;
+    if (p.how == kTiles) p.bytes = 256 + (size_t)p.tiles * p.chains * 64 * (12 * V + 4);
     return p;
 }
 
@@ -555,7 +614,8 @@ template <bool BACK> hipError_t launch(const Gated &a, bool is_bf16, bool aligne
             Work work;
             work.next = reinterpret_cast<uint32_t *>(base);
             work.span = reinterpret_cast<unsigned long long *>(base + 256);
-            work.out = reinterpret_cast<uint32_t *>(base + 256 + words * 8);
+            work.out = base + 256 + words * 8;
+            work.power = reinterpret_cast<uint32_t *>(base + 256 + words * 12);
             const long long count = (long long)p.chains * p.tiles;
             auto kernel = p.farther ? gated_tile_kernel<T, V, vec.value, BACK, mix.value, 2>
                                     : gated_tile_kernel<T, V, vec.value, BACK, mix.value, 1>;
