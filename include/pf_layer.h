@@ -45,7 +45,8 @@ extern "C" {
  *
  * With m = max(max|y| over the block, 1e-30): scale = m / 448, Q = e4m3(y * 448 / m).  At least one of Y and Q is
  * wanted (PF_ERR_NULL).  D up to 16384 (pf_norm_supported; else PF_ERR_UNSUPPORTED).  M == 0: nothing is done, and the
- * pointers may be NULL.  A row of zeros with eps = 0 gives NaN.
+ * pointers may be NULL.  A row of zeros with eps = 0 gives NaN.  Squares are summed in fp32: where their sum overflows (values of
+ * 1e19), y is zero.
  */
 int pf_norm_supported(int D, pf_dtype dt);
 pf_status pf_norm_fwd(const void *X, long long ldx, const void *R, long long ldr, const void *w, void *S, void *Y,

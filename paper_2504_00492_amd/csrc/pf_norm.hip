@@ -95,10 +95,15 @@ __global__ __launch_bounds__(kThreads<G>) void norm_fwd_kernel(NormFwd a)
             if (a.Y) store8<T, VEC>(static_cast<T *>(a.Y) + row * a.D + col(i), rounded<T, VEC>(u * rho), a.D - col(i));
             if (a.Q) {
                 // y * 448 / max|y| = u * 448 / max|u|: the row's factor has no part in the 8 bits
-                const float top = __uint_as_float(top_of_16(top8(u))), ytop = top * rho;
+                float top = __uint_as_float(top_of_16(top8(u))), ytop = top * rho, least = kTop / kLeast;
+                if (top < 0x1p-60f) {      // (next to nothing in a row that is next to nothing: with a small eps these factors leave fp32)
+                    u *= 0x1p64f;
+                    top *= 0x1p64f;
+                    least *= 0x1p-64f;
+                }
                 float inv = 1.f / top * kTop, scale = ytop * (1.f / kTop);
                 if (ytop < kLeast) {
-                    inv = rho * (kTop / kLeast);
+                    inv = rho * least;
                     scale = kLeast / kTop;
                 }
                 if (!(ytop >= 0.f)) inv = ytop;      // NaN
