@@ -105,9 +105,10 @@ pf_status pf_quant_fp8(const void *X, long long ldx, void *Q, long long ldq, flo
  *
  * dt = PF_BF16: the sum over a block is the 8-bit matrix instruction's, which adds eight products at a time aligned to the
  * largest of them and drops what lies 2^-13 below that (1.4e-5 of the result's norm for normally distributed values).
- * dt = PF_F32: exact products, fp32 sums.  Blocks are joined by one fp32 fma each.  The gradient of A's
+ * dt = PF_F32: exact products, fp32 sums.  Blocks are joined by one fp32 fma each, with sa sb, rounded to fp32, as the factor.  The gradient of A's
  * source is the same product on dY and the transposed copy of B, that of B's on the transposed copies of dY and A's source
- * (pf_quant_fp8).  b_rows other than 1 and 128: PF_ERR_UNSUPPORTED.  M == 0 or N == 0: nothing is done; K >= 1.
+ * (pf_quant_fp8).  b_rows other than 1 and 128: PF_ERR_UNSUPPORTED.  M == 0 or N == 0: nothing is done; K from 1 to
+ * 2^31 - 128 (PF_ERR_UNSUPPORTED beyond).
  */
 size_t pf_matmul_fp8_workspace_bytes(int M, int N, int K, int b_rows);
 pf_status pf_matmul_fp8(const void *A, long long lda, const float *sa, const void *B, long long ldb, const float *sb,

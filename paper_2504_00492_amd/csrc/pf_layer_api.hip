@@ -2,6 +2,8 @@
 #include "../../include/pf_layer.h"
 #include "pf_layer_internal.h"
 
+#include <limits.h>
+
 namespace {
 
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -67,9 +69,12 @@ extern "C" pf_status pf_quant_fp8(const void *X, long long ldx, void *Q, long lo
     return launched(pf::launch_quant({X, Q, QT, scale, scaleT, ldx, ldq, ldqt, M, K, rows}, dt == PF_BF16, on(stream)));
 }
 
+// columns of a row are counted in 32 bits, in whole blocks of 128
+static constexpr int kDeepest = INT_MAX - 127;
+
 extern "C" size_t pf_matmul_fp8_workspace_bytes(int M, int N, int K, int b_rows)
 {
-    if (M <= 0 || N <= 0 || K <= 0 || (b_rows != 1 && b_rows != 128)) return 0;
+    if (M <= 0 || N <= 0 || K <= 0 || K > kDeepest || (b_rows != 1 && b_rows != 128)) return 0;
     return pf::matmul_workspace_bytes(M, N, K, b_rows);
 }
 
@@ -78,7 +83,7 @@ extern "C" pf_status pf_matmul_fp8(const void *A, long long lda, const float *sa
                                    size_t workspace_bytes, pf_stream stream)
 {
     if (M < 0 || N < 0 || K <= 0) return PF_ERR_SHAPE;
-    if (!known(dt) || (b_rows != 1 && b_rows != 128)) return PF_ERR_UNSUPPORTED;
+    if (!known(dt) || (b_rows != 1 && b_rows != 128) || K > kDeepest) return PF_ERR_UNSUPPORTED;
     if (M == 0 || N == 0) return PF_OK;
     if (!A || !sa || !B || !sb || !C) return PF_ERR_NULL;
     if (lda < K || ldb < K || lda % 16 || ldb % 16 || ldc < N) return PF_ERR_SHAPE;
