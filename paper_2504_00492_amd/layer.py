@@ -204,6 +204,10 @@ def _workspace(need, given, device):
         if not need:
             return None, None, 0
         given = _empty(need, dtype=torch.uint8, device=device)
+    elif given.device != device:
+        raise ValueError(f"workspace must be on {device}; there is no CPU path")
+    elif not given.is_contiguous():
+        raise ValueError("workspace must be contiguous")
     return given, given.data_ptr(), given.numel() * given.element_size()
 
 

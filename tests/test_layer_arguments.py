@@ -1,0 +1,20 @@
+"""What the functions on tensors (paper_2504_00492_amd.layer) check of workspaces and streams, without a GPU: memory that a kernel could not
+reach, or that is shorter than it counts, is refused before the library's call."""
+import pytest
+import torch
+
+from test_layer_host import layer  # noqa: F401  (fixture)
+
+
+def test_workspace_elsewhere(layer):  # noqa: F811
+    with pytest.raises(ValueError, match="workspace must be on cuda:0"):
+        layer._workspace(64, torch.empty(64, dtype=torch.uint8), torch.device("cuda:0"))
+
+
+def test_workspace_in_pieces(layer):  # noqa: F811
+    """A view that counts more bytes than it has, and one whose bytes are apart."""
+    for t in (torch.empty(1, dtype=torch.uint8).expand(64), torch.empty(128, dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError, match="workspace must be contiguous"):
+            layer._workspace(64, t, torch.device("cpu"))
+    whole = torch.empty(64, dtype=torch.float32)
+    assert layer._workspace(64, whole, torch.device("cpu"))[1:] == (whole.data_ptr(), 256)
