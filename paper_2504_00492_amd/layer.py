@@ -225,14 +225,21 @@ def _call(fn, name, index, *args):
 def _on_stream(f):
     """f with an argument `stream` (a torch stream, or the handle of one; None: the current one).  The call's outputs and workspace
     come from that stream's memory, as if it had been made current: memory of another stream could still be in use there,
-    or be handed out again there before the call is through."""
+    or be handed out again there before the call is through.  What the call reads is the caller's to order and to keep until then, as
+    with a current stream."""
     @functools.wraps(f)
     def with_stream(*args, stream=None, **kwargs):
         if stream is None:
             return f(*args, **kwargs)
+        first = next((t for t in (*args, *kwargs.values()) if isinstance(t, torch.Tensor)), None)
+        if first is None:
+            raise ValueError("there is no tensor whose device the stream could be of")
+        if not first.is_cuda:
+            return f(*args, **kwargs)      # (which says what is wrong with it)
         if isinstance(stream, int):
-            device = next(t for t in args if t is not None).device
-            stream = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
+            stream = torch.cuda.ExternalStream(stream, first.device) if stream else torch.cuda.default_stream(first.device)
+        elif stream.device != first.device:
+            raise ValueError(f"stream must be one of {first.device}")
         with torch.cuda.stream(stream):
             return f(*args, **kwargs)
     return with_stream

@@ -18,3 +18,14 @@ def test_workspace_in_pieces(layer):  # noqa: F811
             layer._workspace(64, t, torch.device("cpu"))
     whole = torch.empty(64, dtype=torch.float32)
     assert layer._workspace(64, whole, torch.device("cpu"))[1:] == (whole.data_ptr(), 256)
+
+
+def test_stream_by_keyword(layer):  # noqa: F811
+    """A stream's handle with all tensors by keyword, and with none."""
+    x = torch.zeros(1, 4, 64)
+    for call in (lambda: layer.gated_fwd(X=x, G=x, stream=0), lambda: layer.norm_fwd(X=x[0], eps=0., stream=5),
+                 lambda: layer.matmul_fp8(A=x[0], sa=x, B=x[0], sb=x, stream=0), lambda: layer.quant_fp8(x[0], stream=0)):
+        with pytest.raises(ValueError, match="no CPU path"):
+            call()
+    with pytest.raises(ValueError, match="no tensor"):
+        layer.quant_fp8(X=None, stream=0)
