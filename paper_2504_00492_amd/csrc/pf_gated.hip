@@ -45,13 +45,21 @@ template <typename T, bool BACK, bool MIX> constexpr int tile_tokens(bool farthe
 
 // the decay a, 1 - a, and d a / d g of a gate's value
 struct Gate { float a, rest, slope; };
-__device__ __forceinline__ float exponential(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+// e^x.  x log2 e is rounded, which is |x| / 2 units of fp32 in the result: of gates in fp32 it is put right (1 x 65536 x 2048 296 -> 298 us), gates in bf16
+// are themselves off by some 2^15 times that.
+template <bool EXACT> __device__ __forceinline__ float exponential(float x)
+{
+    const float t = x * 1.44269504088896341f, y = __builtin_amdgcn_exp2f(t);
+    if constexpr (!EXACT) return y;
+    const float rest = fmaf(x, 1.92596298909109e-8f, fmaf(x, 1.44269504088896341f, -t));
+    return fabsf(t) < 200.f ? fmaf(y, rest * 0.693147180559945309f, y) : y;      // (infinite x: 0 and infinity)
+}
 // what is not used of the result is not computed
-template <int FORM, bool MIX> __device__ __forceinline__ Gate gate_of(float g)
+template <int FORM, bool MIX, bool EXACT> __device__ __forceinline__ Gate gate_of(float g)
 {
     if (FORM == 0) return {g, 1.f - g, 1.f};
     if (FORM == 1) {
-        const float a = exponential(g);
+        const float a = exponential<EXACT>(g);
         float rest = 0.f;
         if (MIX) {      // 1 - e^g: near zero the series, whose first term left out is 2e-8 of it
             float p = 1.f / 5040;
@@ -65,7 +73,7 @@ template <int FORM, bool MIX> __device__ __forceinline__ Gate gate_of(float g)
         }
         return {a, rest, a};
     }
-    const float e = exponential(-fabsf(g)), d = 1.f + e, near = __builtin_amdgcn_rcpf(d);
+    const float e = exponential<EXACT>(-fabsf(g)), d = 1.f + e, near = __builtin_amdgcn_rcpf(d);
     const float s = fmaf(fmaf(-d, near, 1.f), near, near), t = e * s;      // (one step of Newton: 1 / d but for the last rounding)
     return {g < 0.f ? t : s, g < 0.f ? s : t, t * s};
 }
@@ -246,7 +254,7 @@ template <typename K, int N, bool KEPT> struct Span<K, N, KEPT, false> {
         for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Gate k = gate_of<FORM, MIX>(value(g[i], v));
+                const Gate k = gate_of<FORM, MIX, sizeof(T) == 4>(value(g[i], v));
                 const float in = MIX ? k.rest * value(x[i], v) : value(x[i], v), now = s0 + i < c.a.L ? k.a : 1.f;      // (behind the end x is zero)
                 if constexpr (KEPT) a[i][v] = k.a, b[i][v] = in;
                 A[v].times(now);
@@ -268,7 +276,7 @@ template <typename K, int N, bool KEPT> struct Span<K, N, KEPT, false> {
                 if constexpr (KEPT) {
                     v[j] = fmaf(a[i][j], v[j], b[i][j]);
                 } else {
-                    const Gate k = gate_of<FORM, MIX>(value(g[i], j));
+                    const Gate k = gate_of<FORM, MIX, sizeof(T) == 4>(value(g[i], j));
                     v[j] = fmaf(k.a, v[j], MIX ? k.rest * value(x[i], j) : value(x[i], j));
                 }
             }
@@ -305,7 +313,7 @@ template <typename K, int N, bool KEPT> struct Span<K, N, KEPT, true> {
         for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const float a = s0 + i < c.a.L ? gate_of<FORM, false>(value(g[i], v)).a : 1.f;
+                const float a = s0 + i < c.a.L ? gate_of<FORM, false, sizeof(T) == 4>(value(g[i], v)).a : 1.f;
                 A[v].times(a);
                 H[v] = a * (value(dy[i], v) + H[v]);
                 here(A[v].e);
@@ -326,7 +334,7 @@ template <typename K, int N, bool KEPT> struct Span<K, N, KEPT, true> {
             float dx[V], dg[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const Gate k = gate_of<FORM, MIX>(value(g[i], j));
+                const Gate k = gate_of<FORM, MIX, sizeof(T) == 4>(value(g[i], j));
                 const float l = value(dy[i], j) + v[j];
                 float h = t > 0 ? value(y[i], j) : c.a.h0 && j < c.left ? c.a.h0[c.state + c.mine + j] : 0.f;
                 if (MIX) h -= value(x[MIX ? i : 0], j);
