@@ -8,7 +8,8 @@
  * aligned (PF_ERR_ALIGN; of inputs that come with strides: aligned to their elements), the library never allocates, frees or synchronises, work is enqueued on `stream`, every
  * argument check happens on the host before anything is launched, errors are return codes.  Calls that share a workspace
  * or outputs must be ordered by the caller.  Results do not depend on timing: the same call on the same device gives the
- * same bits.  Sums, statistics and states are held in fp32.  In addition
+ * same bits.  A row or sequence in a call of other sizes may take another kernel, or sums in another order, and differ in its last
+ * bits.  Sums, statistics and states are held in fp32.  In addition
  *   - the innermost dimension of every array is contiguous; where a row stride (ld...) is an argument, it is in elements, at
  *     least the row's length (PF_ERR_SHAPE) and otherwise free; batch and token strides are not negative and otherwise free;
  *   - outputs must not overlap inputs, except where an entry says so;
