@@ -101,14 +101,20 @@ __global__ __launch_bounds__(kThreads<G>) void norm_fwd_kernel(NormFwd a)
                     top *= 0x1p64f;
                     least *= 0x1p-64f;
                 }
-                float inv = 1.f / top * kTop, scale = ytop * (1.f / kTop);
+                // 448 / top as two numbers: one alone is off by two roundings, and what lies at the middle of two steps of e4m3 would go
+                // either way
+                const float one = 1.f / top;
+                float inv = one * kTop, rest = fmaf(-inv, top, kTop) * one, scale = ytop * (1.f / kTop);
                 if (ytop < kLeast) {
                     inv = rho * least;
+                    rest = 0.f;
                     scale = kLeast / kTop;
                 }
                 if (!(ytop >= 0.f)) inv = ytop;      // NaN
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = fmaf(u[e], inv, u[e] * rest);
                 if (col(i) < a.D) {
-                    store_e4m3(static_cast<uint8_t *>(a.Q) + row * a.ldq + col(i), to_e4m3(u * inv), a.D - col(i));
+                    store_e4m3(static_cast<uint8_t *>(a.Q) + row * a.ldq + col(i), to_e4m3(u), a.D - col(i));
                     if (lane % 16 == 0) a.scale[(long long)(col(i) / 128) * a.M + row] = scale;
                 }
             }
