@@ -11,16 +11,16 @@
 // channels of one sequence) from tile to tile; else every tile has a workgroup.  A tile tells the (A, H) of its channels as soon as
 // it has read them, looks back for the nearest tile in front whose outgoing values are told (each of its wavefronts listens to one
 // of the eight in front, where there are few chains to two of sixteen), runs these through the (A, H) of the tiles between, and tells
-// its own outgoing values.  A word that is told stands for itself (clear is a pattern that no value has), 8 bytes in one store, so no
-// fence orders anything.  Tiles are handed out by a counter, all chains' first tiles first: a workgroup waits only for tiles handed
+// its own outgoing values.  A word that is told stands for itself (clear is a pattern that no value has), one store of 4 or 8 bytes, so
+// no fence orders anything.  Tiles are handed out by a counter, all chains' first tiles first: a workgroup waits only for tiles handed
 // out before its own, whose workgroups are on the chip already and wait for nothing later, so every wait ends.  What a tile makes of
 // the values that come in depends on the tiles between them in order, whichever were told, so the bits do not depend on timing.
 //
-// Bound by HBM: 1 x 65536 x 4096 forward in bf16 312 us, 5.2 TB/s (a plain copy: 5.1); 1 x 65536 x 2048 in fp32 5.5 TB/s; backward with
-// the mix 2 x 8192 x 4096 183 us, 4.4 TB/s, where the tiles are not long enough for what a tile waits to be hidden.  A long sequence of few
-// channels is bound by the chain, 0.18 us a tile: 1 x 65536 x 64 62 us.  Tried and left: two channels more to a lane (321 -> 375 us), workgroups
-// that draw tile after tile and read ahead (475: what they hold in registers makes tiles short), 16 tiles listened to here too (twice the words
-// to read: 351), four or twelve wavefronts (363, 348).
+// Bound by HBM: 1 x 65536 x 4096 forward in bf16 325 us, 5.0 TB/s (a plain copy: 5.1); 1 x 65536 x 2048 in fp32 298 us, 5.4 TB/s; backward with
+// the mix 2 x 8192 x 4096 192 us, 4.2 TB/s, where the tiles are not long enough for what a tile waits to be hidden.  A long sequence of few
+// channels is bound by the chain, 0.19 us a tile: 1 x 65536 x 64 64 us.  Tried and left, where 1 x 65536 x 4096 took 321 us: two channels more to a
+// lane (375), workgroups that draw tile after tile and read ahead (475: what they hold in registers makes tiles short), 16 tiles listened to
+// here too (twice the words to read: 351), four or twelve wavefronts (363, 348).
 #include "pf_layer_common.h"
 #include "pf_layer_internal.h"
 
@@ -34,8 +34,8 @@ namespace {
 
 constexpr int kWaves = 8, kWalkSteps = 16;
 // Steps of a wavefront's span of a tile, as its registers allow: forward (two arrays) two workgroups to a compute unit, of tiles that are
-// long, so that there is less to tell and to wait for (1 x 65536 x 4096, bf16: 16 steps 351 us, 24 320, 28 311; 32 1 to 4 % more than 28); backward (up to four
-// arrays) three of short ones (2 x 8192 x 4096: two of 16 steps 188 us, three of 9 183; 16 x 2048 x 4096 316 and 314).
+// long, so that there is less to tell and to wait for (1 x 65536 x 4096, bf16: 16 steps 372 us, 24 338, 28 326, 32 329); backward (up to four
+// arrays) three of short ones (2 x 8192 x 4096 with the mix: two of 16 steps 197 us, three of 9 193; 16 x 2048 x 4096 386 and 376).
 template <typename T, bool BACK, bool MIX, bool FARTHER>
 constexpr int kTileSteps = BACK ? (FARTHER ? 16 : 9) : sizeof(T) == 4 ? 32 : FARTHER ? 24 : MIX ? 20 : 28;
 template <typename T, bool BACK, bool MIX> constexpr int tile_tokens(bool farther)
@@ -169,7 +169,6 @@ struct Work {
     void *out;               // [tile][lane] what goes out of its channels, one word
 };
 
-// steps of a chain in the order of the recurrence: step s is token s, or of the backward token L - 1 - s
 // a call's kind: element type, channels a lane, whether these lie in whole words, direction, mix, and the gate's form
 template <typename T_, int V_, bool VEC_, bool BACK_, bool MIX_, int FORM_> struct Kind {
     using T = T_;
@@ -177,6 +176,7 @@ template <typename T_, int V_, bool VEC_, bool BACK_, bool MIX_, int FORM_> stru
     static constexpr bool VEC = VEC_, BACK = BACK_, MIX = MIX_;
 };
 
+// steps of a chain in the order of the recurrence: step s is token s, or of the backward token L - 1 - s
 template <typename T, int V, bool VEC, bool BACK> struct Chain {
     const Gated &a;
     const T *x, *g, *dy, *yin;      // (of the wavefront's first channel: the same for all lanes)
@@ -227,8 +227,8 @@ template <typename T, int V, bool VEC, bool BACK> struct Chain {
 template <typename K, int N, bool KEPT, bool BACK = K::BACK> struct Span;
 
 // Forward: N steps in registers.  Each is needed twice.  KEPT, with the mix, whose gates cost most: a and b stay in registers once they are
-// formed (fp32: in the place of g and x; bf16: twice that, so fewer steps).  2 x 8192 x 4096 in bf16, 24 steps formed twice 111 us, 20 kept
-// 99; 64 x 512 x 2048 107 and 90; 3 x 4099 x 1001 in fp32 45.5 and 43.0.  Without the mix they are formed twice.
+// formed (fp32: in the place of g and x; bf16: twice that, so fewer steps).  2 x 8192 x 4096 in bf16, 24 steps formed twice 118 us, 20 kept
+// 106; 64 x 512 x 2048 96 and 90; 3 x 4099 x 1001 in fp32 51 and 47.  Without the mix they are formed twice.
 template <typename K, int N, bool KEPT> struct Span<K, N, KEPT, false> {
     using T = typename K::T;
     static constexpr int V = K::V, FORM = K::FORM;
@@ -586,8 +586,8 @@ Plan plan(int B, int L, int D, bool is_bf16, bool back, bool mix)
     p.groups = (int)((D + 64LL * V - 1) / (64 * V));
     p.chains = (int)std::min((long long)B * p.groups, (long long)INT_MAX);      // (launch refuses as many)
     // Few chains have many of their tiles on the chip at once: listening to sixteen, and backward tiles of 16 steps, two workgroups to a
-    // compute unit, make a long sequence's chain shorter: 1 x 65536 in bf16, forward 64 channels 77 -> 62 us, 512: 91 -> 75, 1024: 107 -> 110;
-    // backward 64: 188 -> 89, 512: 209 -> 110, 1024: 234 -> 173, 1 x 16384 x 512 67 -> 42, 1 x 3000 x 512 with the mix 20 -> 22.
+    // compute unit, make a long sequence's chain shorter: 1 x 65536 in bf16, forward 64 channels 69 -> 64 us, 512: 83 -> 76, 1024: 104 -> 116;
+    // backward 64: 174 -> 87, 512: 193 -> 109, 1024: 215 -> 182, 1 x 16384 x 512 64 -> 43; where tiles are few, 1 x 3000 x 512 with the mix, 20 -> 22.
     p.farther = p.chains <= (back ? 8 : 6);
     auto tiles = [&] {
         const int tile = back ? tile_tokens<bf16, true, false>(p.farther) : !is_bf16 ? tile_tokens<float, false, false>(p.farther)

@@ -10,7 +10,8 @@
 // 8192 x 8192 x 8192 into bf16: 450 us, 2450 TFLOP/s, 89 % of what the library's product of 8-bit matrices without scales reaches
 // (2765), and 405 us with the scales left out, so they cost 10 %; the matrix units are busy 63 % of the time at the 1.87 GHz that the
 // card's power then allows.  Into fp32, a scale for every row of both: 4096 x 4096 x 8192 254 us, 1080 TFLOP/s, bound by turning the
-// values to bf16 in the vector units (the library's bf16 product: 1390).  Three rows of A, 20544 x 4096: 19.9 us, 4.2 TB/s.
+// values to bf16 in the vector units (the library's bf16 product: 1390).  Three rows of A, 20544 x 4096: 19.9 us, 4.2 TB/s
+// (20.3, 4.1, with eight sets of weights in turn, 670 MB, which the last-level cache does not hold).
 // A lane (r = l & 15, g = l >> 4) holds 32 values of row r of either operand; which 32 does not matter as long as both
 // agree: the 16 bytes from 16 g on and from 64 + 16 g on.  B's rows are the first operand and A's the second, so that a lane's four
 // results, rows 4 g .. 4 g + 3 of column r, lie side by side in C.
@@ -424,12 +425,17 @@ constexpr int kTileRows[6] = {256, 128, 64, 128, 64, 128}, kTileCols[6] = {256, 
 struct Plan { int tile, splits, cols; };
 
 // The cheapest by a model of each, in us, fitted to calls on an MI355X of 256 compute units (clocks differ by some per cent from
-// card to card; what it picked was within 8 % of the best of all for 17 sizes from 32 x 20544 x 4096 to 8192 x 64 x 4096, either type):
+// card to card).  Of all tiles and splits, timed for 17 sizes from 1 x 4096 x 4096 to 4096 x 4096 x 8192, it picked the best or one within 5 %,
+// but for 128 x 4096 x 4096 in bf16, 17.5 us instead of 15.9, and 16 x 20544 x 4096:
 //   tiles      rounds of as many workgroups as a compute unit holds, each 1.5 us and so much a block of K, by how many
 //              share a compute unit; splits add the join: 4 us and their sums to memory and back
 //   few rows   B at 5 TB/s and the rows of A, read for every 16 rows of B, at 12 TB/s
+// Up to 16 rows of A it is always the kernel for few rows, which needs no workspace: 1 x 4096 x 4096 6.7 us (the best tiles: 11.1), 16 x 4096 x
+// 4096 7.5 (11.8), 16 x 1024 x 8192 11.6 (12.0), but 16 x 20544 x 4096 26.5 (22.7 with K in four parts, 25.1 in one).
 // Of tiles of 256 columns, a last column of tiles of which at most a quarter is there is left, where that is cheaper: the tiles of
-// 8192 x 20544 x 4096 are 10.1 rounds of workgroups, without the last 64 columns 10.
+// 8192 x 20544 x 4096 are 10.1 rounds of workgroups, without the last 64 columns 10: 615 us instead of 641; 8192 x 2112 x 1024 30.3 instead of
+// 36.4, 4096 x 4160 x 4096 73 instead of 102, 16384 x 1088 x 4096 84 instead of 102; 2048 x 4160 x 2048 stays whole, 30.2 either way.  Half a
+// column left would pay too (8192 x 4192 x 4096 135 instead of 155, 8192 x 4224 x 4096 138 instead of 157).
 Plan plan_of(int M, int N, int K, bool exact, double *cost = nullptr)
 {
     // us a block of K of 1, 2, 3 workgroups a compute unit

@@ -5,7 +5,7 @@
 // the width alone: up to 128 columns a row to 16 lanes, four rows to a wavefront, and no barrier up to 1024 columns.
 //
 // Bound by HBM (a plain copy reaches 5.1 TB/s): forward 32768 x 4096, residual in, sum and 8 bits out, bf16, 174 us, 5.4 TB/s; 262144 x 128 into
-// bf16 21.7 us, 6.2; backward 8191 x 4096 49.3 us and 4.1 for the sums of dw, 5.0 TB/s; a few rows: 3.5 us, what a launch takes.
+// bf16 21.2 us, 6.3; backward 8191 x 4096 48.5 us and 4.1 for the sums of dw, 5.0 TB/s; a few rows: 3.8 us, what a launch takes.
 #include "pf_layer_common.h"
 #include "pf_layer_internal.h"
 
