@@ -91,7 +91,7 @@ def _lengths(case):
     g.manual_seed(case["B"] * 1000003 + case["L"] * 1009 + case["tokens"])
     n = (torch.rand(case["B"], generator=g) * (case["L"] + 1)).long().clamp(max=case["L"])
     n = n * min(case["tokens"], int(n.sum())) // max(1, int(n.sum()))
-    n[0] = max(1, n[0])
+    n[0] += int(n.sum()) == 0
     return n
 
 
