@@ -1,7 +1,8 @@
 /*
  * pf_layer.h - C ABI of the operators of a layer around the delta rule of pf.h, MI355X (gfx950): the norm in front of
  *              its projections, the projections in 8 bits, and the gated linear recurrence, which is the flow of
- *              Section 3.1 of ParallelFlow (arXiv 2504.00492) with diagonal drivers.  Forward and backward.
+ *              Section 3.1 of ParallelFlow (arXiv 2504.00492) with diagonal drivers; the norm of heads with the rotation by
+ *              position, and the delta rule with a gate.  Forward and backward.
  *              Library: libpf_layer.so (it loads libpf.so for pf_status_str and pf_version).
  *
  * Conventions: those of pf.h.  Every data pointer is a DEVICE pointer owned by the caller, base addresses are 16-byte
@@ -168,6 +169,132 @@ pf_status pf_gated_bwd(const void *X, long long xb, long long xt, const void *G,
                        const float *h0, const void *Y, const void *dY, long long dyb, long long dyt, const float *dhL,
                        void *dX, void *dG, float *dh0, int B, int L, int D, pf_gate gate, int mix, pf_dtype dt,
                        void *workspace, size_t workspace_bytes, pf_stream stream);
+
+/*
+ * Norm of every head of queries and keys, and the rotation of each by its token's position, in one pass:
+ *
+ *   n = sqrt(mean(x^2) + eps)  (PF_NORM_RMS)   or   sqrt(sum(x^2) + eps)  (PF_NORM_L2)        over a head's d values
+ *   y = scale * turn(x / n * w)                scale = q_scale for queries, 1 for keys
+ *
+ * turn leaves the values from the rot-th on as they are and turns rot / 2 pairs of the others, pair i by the angle whose cosine and
+ * sine are table[p][i] and table[p][rot / 2 + i] at the token's position p:
+ * (a, b) -> (a cos - b sin, a sin + b cos), with a, b = values i and i + rot / 2 (pairs = 0) or 2 i and 2 i + 1 (pairs = 1).
+ *
+ *   Q          [M, Hq, d], strides qt (token), qh (head)   dt     in    Hq == 0, Hk == 0: there are none of these
+ *   K          [M, Hk, d], strides kt, kh                  dt     in
+ *   wq, wk     [d]                                         dt     in    NULL: ones
+ *   table      [far, rot]                                  fp32   in    not read where rot == 0, as the positions
+ *   positions  [M]                                         int    in    a position that the table does not have gives NaN
+ *   Yq, Yk     [M, Hq, d], [M, Hk, d]                      dt     out   Yq == Q, Yk == K is allowed where these are dense
+ *
+ * rot is even, from 0 to d.  ceil(rot / 8) + ceil((d - rot) / 8) up to 64 (pf_head_norm_supported; else PF_ERR_UNSUPPORTED): d up to 504 at
+ * least, 512 where 8 divides rot.  M == 0: nothing is done.  Squares are summed in fp32 (as in pf_norm_fwd).
+ */
+typedef enum { PF_NORM_RMS = 0, PF_NORM_L2 = 1 } pf_norm_kind;
+
+int pf_head_norm_supported(int d, int rot, pf_dtype dt);
+pf_status pf_head_norm_fwd(const void *Q, long long qt, long long qh, const void *K, long long kt, long long kh,
+                           const void *wq, const void *wk, const float *table, int far, const int *positions, void *Yq,
+                           void *Yk, int M, int Hq, int Hk, int d, int rot, pf_norm_kind kind, int pairs, float eps,
+                           float q_scale, pf_dtype dt, pf_stream stream);
+
+/*
+ * Its backward.  With xh = x / n, t = scale * the gradient turned back and g = w t:
+ *
+ *   dx = (g - xh m) / n ,  m = mean(g xh) (PF_NORM_RMS) or sum(g xh) (PF_NORM_L2) ,     dw = sum over tokens and heads of t xh
+ *
+ *   dYq, dYk   [M, Hq, d], [M, Hk, d], strides ..t, ..h    dt     in
+ *   dQ, dK     [M, Hq, d], [M, Hk, d]                      dt     out   dQ == dYq or dQ == Q (dK ..) is allowed where that is dense
+ *   dwq, dwk   [d]                                         fp32   out   NULL: not wanted (neither: no workspace).  No rows: zeros
+ *   workspace / workspace_bytes                            at least pf_head_norm_bwd_workspace_bytes(...) bytes, overwritten
+ */
+size_t pf_head_norm_bwd_workspace_bytes(int M, int Hq, int Hk, int d, int rot);
+pf_status pf_head_norm_bwd(const void *Q, long long qt, long long qh, const void *K, long long kt, long long kh,
+                           const void *dYq, long long dyqt, long long dyqh, const void *dYk, long long dykt, long long dykh,
+                           const void *wq, const void *wk, const float *table, int far, const int *positions, void *dQ,
+                           void *dK, float *dwq, float *dwk, int M, int Hq, int Hk, int d, int rot, pf_norm_kind kind,
+                           int pairs, float eps, float q_scale, pf_dtype dt, void *workspace, size_t workspace_bytes,
+                           pf_stream stream);
+
+/*
+ * Gated delta rule: pf_delta_fwd's recurrence at r = 1 with a gate for every token and head, per sequence and head from S_0 = S0,
+ *
+ *   S_t = a_t S_{t-1} (I - beta_t k_t k_t^T) + beta_t v_t k_t^T ,   o_t = S_t q_t ,   a_t = exp(g_t)         t = 1 .. L
+ *
+ * computed in chunks of 64 tokens.  Hv heads of values, gates and states; each Hv / Hk of them that follow one another share a head of
+ * queries and keys.  beta and g are used as given, keys are not normalised, q is not scaled (pf_head_norm_fwd does both).  g below -256
+ * counts as -256, where a is 0 (a sequence anew, in finite numbers); above 256 as 256, where a is infinite.
+ *
+ *   Q        [N, L, Hk, d_k], strides qb (sequence), qt (token), qh (head)   dt     in
+ *   K        [N, L, Hk, d_k], strides kb, kt, kh                             dt     in
+ *   V        [N, L, Hv, d_v], strides vb, vt, vh                             dt     in
+ *   G, beta  [N, L, Hv], strides gb, gt, gh and bb, bt, bh                   dt     in    g and beta
+ *   S0       [N, Hv, d_v, d_k]                                               fp32   in    NULL: zeros
+ *   offsets  [N + 1]                                                         int    in    packed sequences, or NULL (below)
+ *   O        [N, L, Hv, d_v]                                                 dt     out
+ *   SL       [N, Hv, d_v, d_k]                                               fp32   out   NULL: not written.  SL == S0 is allowed
+ *   workspace / workspace_bytes   at least pf_gated_delta_workspace_bytes(..., backward = 0, dt) bytes, overwritten; what it holds
+ *                                 before does not matter, and nothing in it is kept from call to call
+ *
+ * Packed sequences: Q, K, V, G, beta and O are [L, ...], the rows of all sequences one behind the other (the sequence strides are not looked
+ * at), and sequence n is rows offsets[n] .. offsets[n + 1] - 1, any number of them, none too.  Rows that belong to no sequence are
+ * neither read nor written.  Offsets are in device memory and are not checked on the host; one below its predecessors counts as the
+ * largest of these, negative ones as 0, ones beyond L as L.
+ *
+ * Heads: Hk divides Hv; d_k and d_v up to 256 (pf_gated_delta_supported; else PF_ERR_UNSUPPORTED, Hv not a multiple of Hk: PF_ERR_SHAPE).
+ * States and all that goes into them are computed in fp32 (24 bits); what goes into O alone with 16 bits at least for dt = PF_BF16.  L up to
+ * 2^30.  No tokens: SL receives S0 (or zeros), and the sequence pointers may be NULL.  N == 0: nothing is done.
+ * NaN and infinities in a token reach all later ones, and may reach the outputs of those up to 63 before it whose chunk it shares.
+ */
+int pf_gated_delta_supported(int Hk, int Hv, int d_k, int d_v, pf_dtype dt);
+size_t pf_gated_delta_workspace_bytes(int N, int L, int Hk, int Hv, int d_k, int d_v, int packed, int backward, pf_dtype dt);
+pf_status pf_gated_delta_fwd(const void *Q, long long qb, long long qt, long long qh, const void *K, long long kb, long long kt,
+                             long long kh, const void *V, long long vb, long long vt, long long vh, const void *G, long long gb,
+                             long long gt, long long gh, const void *beta, long long bb, long long bt, long long bh,
+                             const float *S0, const int *offsets, void *O, float *SL, int N, int L, int Hk, int Hv, int d_k,
+                             int d_v, pf_dtype dt, void *workspace, size_t workspace_bytes, pf_stream stream);
+
+/*
+ * Its backward, from the inputs alone: the states are computed again.  With R_L = dSL and R_t the gradient of S_t,
+ *
+ *   R_t <- R_t + do_t q_t^T ,   dq_t = S_t^T do_t ,   e_t = v_t - a_t S_{t-1} k_t ,   dbeta_t = e_t . R_t k_t ,   dv_t = beta_t R_t k_t ,
+ *   dk_t = beta_t R_t^T e_t - a_t S_{t-1}^T dv_t ,   R_t' = R_t - dv_t k_t^T ,   dg_t = a_t <R_t', S_{t-1}> ,   R_{t-1} = a_t R_t' ;   dS0 = R_0
+ *
+ * with dq and dk summed over the heads that share them.  (A g beyond -256 or 256 has the gradient of the bound that it counts as.)
+ *
+ *   dO        [N, L, Hv, d_v], strides ob, ot, oh          dt     in
+ *   dSL       [N, Hv, d_v, d_k]                            fp32   in    NULL: zeros
+ *   dQ, dK    [N, L, Hk, d_k]                              dt     out
+ *   dV        [N, L, Hv, d_v]                              dt     out
+ *   dG, dbeta [N, L, Hv]                                   dt     out
+ *   dS0       [N, Hv, d_v, d_k]                            fp32   out   NULL: not written.  dS0 == dSL is allowed
+ *   workspace / workspace_bytes                            ..., backward = 1: for every 64 tokens and head of 128 x 128 about 230 KB
+ */
+pf_status pf_gated_delta_bwd(const void *Q, long long qb, long long qt, long long qh, const void *K, long long kb, long long kt,
+                             long long kh, const void *V, long long vb, long long vt, long long vh, const void *G, long long gb,
+                             long long gt, long long gh, const void *beta, long long bb, long long bt, long long bh,
+                             const void *dO, long long ob, long long ot, long long oh, const float *S0, const float *dSL,
+                             const int *offsets, void *dQ, void *dK, void *dV, void *dG, void *dbeta, float *dS0, int N, int L,
+                             int Hk, int Hv, int d_k, int d_v, pf_dtype dt, void *workspace, size_t workspace_bytes, pf_stream stream);
+
+/*
+ * One token of B sequences, whose states are in a pool and are changed in place.
+ *
+ *   Q, K     [B, Hk, d_k], strides qb, qh and kb, kh       dt     in
+ *   V        [B, Hv, d_v], strides vb, vh                  dt     in
+ *   G, beta  [B, Hv], strides gb, gh and bb, bh            dt     in
+ *   S        [pool, Hv, d_v, d_k]                          fp32   in/out
+ *   slots    [B]                                           int    in    state of each sequence; NULL: b.  A sequence whose slot is not
+ *                                                                       from 0 to pool - 1 (-1: padding), or is that of a sequence
+ *                                                                       before it, has no state: its o is 0 and nothing else happens
+ *   O        [B, Hv, d_v]                                  dt     out
+ *
+ * pool at least B without slots (PF_ERR_SHAPE).  All in fp32.  B == 0: nothing is done.
+ */
+pf_status pf_gated_delta_step(const void *Q, long long qb, long long qh, const void *K, long long kb, long long kh, const void *V,
+                              long long vb, long long vh, const void *G, long long gb, long long gh, const void *beta,
+                              long long bb, long long bh, float *S, const int *slots, void *O, int B, int pool, int Hk, int Hv,
+                              int d_k, int d_v, pf_dtype dt, pf_stream stream);
 
 #ifdef __cplusplus
 }

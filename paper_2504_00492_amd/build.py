@@ -14,7 +14,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpf.so")
 # the operators around the delta rule, a library of their own: who runs the recurrence alone does not load them
 LAYER_LIB = os.path.join(HERE, "libpf_layer.so")
-LAYER_SOURCES = ["pf_layer_api.hip", "pf_norm.hip", "pf_quant.hip", "pf_matmul.hip", "pf_gated.hip"]
+LAYER_SOURCES = ["pf_layer_api.hip", "pf_norm.hip", "pf_quant.hip", "pf_matmul.hip", "pf_gated.hip", "pf_heads.hip",
+                 "pf_gdelta_flow.hip", "pf_gdelta_scan.hip", "pf_gdelta_grad.hip", "pf_gdelta_step.hip"]
 SOURCES = ["pf_api.hip", "pf_generic.hip", "pf_flow.hip", "pf_scan.hip", "pf_fused.hip", "pf_segments.hip", "pf_sigdelta.hip", "pf_rescale.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Packed-fp32 VALU forms are switched off for every kernel of this library.  The feature flag

@@ -68,4 +68,72 @@ size_t gated_workspace_bytes(int B, int L, int D, bool is_bf16);
 hipError_t launch_gated_fwd(const Gated &a, bool is_bf16, hipStream_t stream);
 hipError_t launch_gated_bwd(const Gated &a, bool is_bf16, hipStream_t stream);
 
+// ---- gated delta rule (pf_gdelta_flow.hip, pf_gdelta_scan.hip, pf_gdelta_grad.hip)
+constexpr int kGDeltaChunk = 64, kGDeltaWidest = 256;
+struct GDelta {
+    const void *Q, *K, *V, *G, *beta, *dO;      // dO: backward
+    long long qb, qt, qh, kb, kt, kh, vb, vt, vh, gb, gt, gh, bb, bt, bh, ob, ot, oh;      // strides: sequence, token, head
+    const float *S0, *dSL;
+    void *O, *dQ, *dK, *dV, *dG, *dbeta;
+    float *SL, *dS0;
+    const int *offsets;      // packed sequences: [N + 1]
+    int N, L, Hk, Hv, dk, dv;      // L: tokens of every sequence, or rows of all packed ones together
+    long long rows;          // rows of the outputs from one sequence to the next (packed: none)
+    int per, chunks;         // chunks of a sequence (not of packed ones) and all together, or as many as there can be
+    int *plan;               // the workspace's parts, set by gdelta_workspace
+    float *T, *P, *vec, *S, *U, *Z, *R;
+};
+// d_k is padded with zeros to a width that the kernels have
+__host__ __device__ inline int gdelta_width(int dk) { return dk <= 64 ? 64 : dk <= 128 ? 128 : 256; }
+// values of one state in the workspace (the backward puts 64 rows of d_k in its place)
+__host__ __device__ inline long long gdelta_state(const GDelta &a) { return (long long)gdelta_width(a.dk) * (a.dv <= 64 ? 64 : (a.dv + 31) / 32 * 32); }
+// whether rows of Q and K are whole widths at multiples of 16 bytes
+inline bool gdelta_full(const GDelta &a, int size)
+{
+    const uintptr_t all = reinterpret_cast<uintptr_t>(a.Q) | reinterpret_cast<uintptr_t>(a.K) | (uintptr_t)((a.qb | a.qt | a.qh | a.kb | a.kt | a.kh) * size);
+    return a.dk == gdelta_width(a.dk) && all % 16 == 0;
+}
+// Bytes of the workspace; a's parts of it, where `at` is not NULL.
+size_t gdelta_workspace(GDelta &a, bool backward, void *at);
+hipError_t launch_gdelta_fwd(const GDelta &a, bool is_bf16, hipStream_t stream);
+hipError_t launch_gdelta_bwd(const GDelta &a, bool is_bf16, hipStream_t stream);
+hipError_t launch_gdelta_flow(const GDelta &a, bool is_bf16, hipStream_t stream);
+hipError_t launch_gdelta_scan(const GDelta &a, bool is_bf16, bool backward, hipStream_t stream);      // backward: leaves states and U
+hipError_t launch_gdelta_scan_bwd(const GDelta &a, bool is_bf16, hipStream_t stream);
+hipError_t launch_gdelta_grad(const GDelta &a, bool is_bf16, hipStream_t stream);
+
+// ---- one token of the gated delta rule (pf_gdelta_step.hip)
+struct GDeltaStep {
+    const void *Q, *K, *V, *G, *beta;
+    long long qb, qh, kb, kh, vb, vh, gb, gh, bb, bh;
+    float *S;
+    const int *slots;
+    void *O;
+    int B, pool, Hk, Hv, dk, dv;
+};
+hipError_t launch_gdelta_step(const GDeltaStep &a, bool is_bf16, hipStream_t stream);
+
+// ---- norm and rotation of heads (pf_heads.hip)
+constexpr int kHeadUnits = 64;      // lanes that a row can take
+inline int head_units(int d, int rot) { return (rot / 2 + 3) / 4 + (d - rot + 7) / 8; }
+struct HeadSide {
+    const void *X, *w, *dY;
+    void *Y;                 // the output; of the backward: dX
+    float *dw;
+    long long xt, xh, dyt, dyh;      // strides: token, head
+    int H;
+    float scale;
+};
+struct Heads {
+    HeadSide side[2];        // queries, keys
+    const float *table;
+    const int *positions;
+    float *part;             // backward: sums for dw, [2][heads_bwd_parts][d]
+    int M, d, rot, far, pairs, l2;
+    float eps;
+};
+int heads_bwd_parts(int M, int Hq, int Hk, int d, int rot);
+hipError_t launch_heads_fwd(const Heads &a, bool is_bf16, hipStream_t stream);
+hipError_t launch_heads_bwd(const Heads &a, bool is_bf16, hipStream_t stream);
+
 }  // namespace pf

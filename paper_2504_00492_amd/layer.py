@@ -19,9 +19,13 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libpf_laye
 
 PF_GATE_VALUE, PF_GATE_LOG, PF_GATE_LOGIT = range(3)
 GATES = {"value": PF_GATE_VALUE, "log": PF_GATE_LOG, "logit": PF_GATE_LOGIT}
+PF_NORM_RMS, PF_NORM_L2 = range(2)
+NORMS = {"rms": PF_NORM_RMS, "l2": PF_NORM_L2}
 
 EXPORTS = ["pf_norm_supported", "pf_norm_fwd", "pf_norm_bwd_workspace_bytes", "pf_norm_bwd", "pf_quant_fp8",
-           "pf_matmul_fp8_workspace_bytes", "pf_matmul_fp8", "pf_gated_workspace_bytes", "pf_gated_fwd", "pf_gated_bwd"]
+           "pf_matmul_fp8_workspace_bytes", "pf_matmul_fp8", "pf_gated_workspace_bytes", "pf_gated_fwd", "pf_gated_bwd",
+           "pf_head_norm_supported", "pf_head_norm_fwd", "pf_head_norm_bwd_workspace_bytes", "pf_head_norm_bwd",
+           "pf_gated_delta_supported", "pf_gated_delta_workspace_bytes", "pf_gated_delta_fwd", "pf_gated_delta_bwd", "pf_gated_delta_step"]
 
 
 def _load() -> ctypes.CDLL:
@@ -40,7 +44,16 @@ def _load() -> ctypes.CDLL:
             ("pf_matmul_fp8", i, [vp, ll, vp, vp, ll, vp, i, vp, ll, i, i, i, i, vp, sz, vp]),
             ("pf_gated_workspace_bytes", sz, [i, i, i, i]),
             ("pf_gated_fwd", i, [vp, ll, ll, vp, ll, ll, vp, vp, vp, i, i, i, i, i, i, vp, sz, vp]),
-            ("pf_gated_bwd", i, [vp, ll, ll, vp, ll, ll, vp, vp, vp, ll, ll, vp, vp, vp, vp, i, i, i, i, i, i, vp, sz, vp])):
+            ("pf_gated_bwd", i, [vp, ll, ll, vp, ll, ll, vp, vp, vp, ll, ll, vp, vp, vp, vp, i, i, i, i, i, i, vp, sz, vp]),
+            ("pf_head_norm_supported", i, [i, i, i]),
+            ("pf_head_norm_fwd", i, [vp, ll, ll] * 2 + [vp, vp, vp, i, vp, vp, vp, i, i, i, i, i, i, i, f, f, i, vp]),
+            ("pf_head_norm_bwd_workspace_bytes", sz, [i, i, i, i, i]),
+            ("pf_head_norm_bwd", i, [vp, ll, ll] * 4 + [vp, vp, vp, i, vp, vp, vp, vp, vp, i, i, i, i, i, i, i, f, f, i, vp, sz, vp]),
+            ("pf_gated_delta_supported", i, [i, i, i, i, i]),
+            ("pf_gated_delta_workspace_bytes", sz, [i, i, i, i, i, i, i, i, i]),
+            ("pf_gated_delta_fwd", i, [vp, ll, ll, ll] * 5 + [vp, vp, vp, vp, i, i, i, i, i, i, i, vp, sz, vp]),
+            ("pf_gated_delta_bwd", i, [vp, ll, ll, ll] * 6 + [vp] * 9 + [i, i, i, i, i, i, i, vp, sz, vp]),
+            ("pf_gated_delta_step", i, [vp, ll, ll] * 5 + [vp, vp, vp, i, i, i, i, i, i, i, vp])):
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = res, args
     return lib
@@ -99,12 +112,62 @@ def pf_gated_bwd(X, xb, xt, G, gb, gt, h0, Y, dY, dyb, dyt, dhL, dX, dG, dh0, B,
                                  _stream_handle(stream)))
 
 
+def pf_head_norm_supported(d, rot, dt) -> int:
+    return int(_lib.pf_head_norm_supported(d, rot, dt))
+
+
+def pf_head_norm_fwd(Q, qt, qh, K, kt, kh, wq, wk, table, far, positions, Yq, Yk, M, Hq, Hk, d, rot, kind, pairs, eps, q_scale, dt,
+                     stream=None) -> int:
+    return int(_lib.pf_head_norm_fwd(_ptr(Q), qt, qh, _ptr(K), kt, kh, _ptr(wq), _ptr(wk), _ptr(table), far, _ptr(positions), _ptr(Yq),
+                                     _ptr(Yk), M, Hq, Hk, d, rot, kind, pairs, eps, q_scale, dt, _stream_handle(stream)))
+
+
+def pf_head_norm_bwd_workspace_bytes(M, Hq, Hk, d, rot) -> int:
+    return int(_lib.pf_head_norm_bwd_workspace_bytes(M, Hq, Hk, d, rot))
+
+
+def pf_head_norm_bwd(Q, qt, qh, K, kt, kh, dYq, dyqt, dyqh, dYk, dykt, dykh, wq, wk, table, far, positions, dQ, dK, dwq, dwk, M, Hq, Hk, d,
+                     rot, kind, pairs, eps, q_scale, dt, workspace, workspace_bytes, stream=None) -> int:
+    return int(_lib.pf_head_norm_bwd(_ptr(Q), qt, qh, _ptr(K), kt, kh, _ptr(dYq), dyqt, dyqh, _ptr(dYk), dykt, dykh, _ptr(wq), _ptr(wk),
+                                     _ptr(table), far, _ptr(positions), _ptr(dQ), _ptr(dK), _ptr(dwq), _ptr(dwk), M, Hq, Hk, d, rot, kind,
+                                     pairs, eps, q_scale, dt, _ptr(workspace), workspace_bytes, _stream_handle(stream)))
+
+
+def pf_gated_delta_supported(Hk, Hv, dk, dv, dt) -> int:
+    return int(_lib.pf_gated_delta_supported(Hk, Hv, dk, dv, dt))
+
+
+def pf_gated_delta_workspace_bytes(N, L, Hk, Hv, dk, dv, packed, backward, dt) -> int:
+    return int(_lib.pf_gated_delta_workspace_bytes(N, L, Hk, Hv, dk, dv, packed, backward, dt))
+
+
+def pf_gated_delta_fwd(Q, qb, qt, qh, K, kb, kt, kh, V, vb, vt, vh, G, gb, gt, gh, beta, bb, bt, bh, S0, offsets, O, SL, N, L, Hk, Hv, dk,
+                       dv, dt, workspace, workspace_bytes, stream=None) -> int:
+    return int(_lib.pf_gated_delta_fwd(_ptr(Q), qb, qt, qh, _ptr(K), kb, kt, kh, _ptr(V), vb, vt, vh, _ptr(G), gb, gt, gh, _ptr(beta), bb,
+                                       bt, bh, _ptr(S0), _ptr(offsets), _ptr(O), _ptr(SL), N, L, Hk, Hv, dk, dv, dt, _ptr(workspace),
+                                       workspace_bytes, _stream_handle(stream)))
+
+
+def pf_gated_delta_bwd(Q, qb, qt, qh, K, kb, kt, kh, V, vb, vt, vh, G, gb, gt, gh, beta, bb, bt, bh, dO, ob, ot, oh, S0, dSL, offsets, dQ,
+                       dK, dV, dG, dbeta, dS0, N, L, Hk, Hv, dk, dv, dt, workspace, workspace_bytes, stream=None) -> int:
+    return int(_lib.pf_gated_delta_bwd(_ptr(Q), qb, qt, qh, _ptr(K), kb, kt, kh, _ptr(V), vb, vt, vh, _ptr(G), gb, gt, gh, _ptr(beta), bb,
+                                       bt, bh, _ptr(dO), ob, ot, oh, _ptr(S0), _ptr(dSL), _ptr(offsets), _ptr(dQ), _ptr(dK), _ptr(dV),
+                                       _ptr(dG), _ptr(dbeta), _ptr(dS0), N, L, Hk, Hv, dk, dv, dt, _ptr(workspace), workspace_bytes,
+                                       _stream_handle(stream)))
+
+
+def pf_gated_delta_step(Q, qb, qh, K, kb, kh, V, vb, vh, G, gb, gh, beta, bb, bh, S, slots, O, B, pool, Hk, Hv, dk, dv, dt,
+                        stream=None) -> int:
+    return int(_lib.pf_gated_delta_step(_ptr(Q), qb, qh, _ptr(K), kb, kh, _ptr(V), vb, vh, _ptr(G), gb, gh, _ptr(beta), bb, bh, _ptr(S),
+                                        _ptr(slots), _ptr(O), B, pool, Hk, Hv, dk, dv, dt, _stream_handle(stream)))
+
+
 # ---- on torch tensors
 #
 # A small call is bound by what happens here (a launch alone takes the host 3.4 us), so every tensor is looked at in as few
 # steps as tell that it is right; _refuse finds out what is wrong with one that is not.
 
-_BF, _F32, _E4 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
+_BF, _F32, _E4, _I32 = torch.bfloat16, torch.float32, torch.float8_e4m3fn, torch.int32
 _DT = {_BF: PF_BF16, _F32: PF_F32}
 _empty, _like, _stream, _current = torch.empty, torch.empty_like, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
@@ -124,7 +187,7 @@ def _first(t, what, dims):
     if not t.is_cuda:
         raise ValueError(f"{what} must be a CUDA (HIP) tensor; there is no CPU path")
     if t.dim() != dims:
-        raise ValueError(f"{what} must have {('two', 'three')[dims - 2]} dimensions")
+        raise ValueError(f"{what} must have {('two', 'three', 'four')[dims - 2]} dimensions")
     dt = _DT.get(t.dtype)
     if dt is None:
         raise ValueError(f"{what} must be float32 or bfloat16")
@@ -402,3 +465,171 @@ def gated_bwd(X, G, Y, dY, h0=None, dhL=None, *, gate: str = "log", mix: bool = 
     _call(_lib.pf_gated_bwd, "pf_gated_bwd", index, *x, *g, hp, yp, *dy, ep, dX.data_ptr(), dG.data_ptr(), dh0.data_ptr(), B, L, D,
           form, bool(mix), dt, kp, kb)
     return dX, dG, dh0
+
+
+def _strided(t, what, shape, dtype, index):
+    """Address and strides, but the innermost, of an array whose innermost dimension is contiguous."""
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
+        _refuse(t, what, shape, dtype, index)
+    *strides, last = t.stride()
+    if last != 1 and shape[-1] > 1:
+        _inner(t, what)
+    return t.data_ptr(), *strides
+
+
+def _free(t, what, shape, dtype, index):
+    """Address and all strides."""
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
+        _refuse(t, what, shape, dtype, index)
+    return t.data_ptr(), *t.stride()
+
+
+def rotary_table(length: int, rot: int, *, base: float = 10000.0, device="cuda"):
+    """Cosines and sines of positions 0 .. length - 1 for head_norm_fwd, [length, rot] in float32: pair i turns by base^(-2 i / rot)
+    for each position (angles in float64, since those of far positions need more than 24 bits)."""
+    turn = torch.arange(length, dtype=torch.float64)[:, None] * base ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)
+    return torch.cat((turn.cos(), turn.sin()), 1).float().to(device)
+
+
+def _heads_of(Q, K, wq, wk, table, positions, norm):
+    """What head_norm_fwd and head_norm_bwd check alike: type code, device index, sizes and the arguments from Q on."""
+    dt, index = _first(Q, "Q", 3)
+    if norm not in NORMS:
+        raise ValueError(f"norm must be one of {', '.join(NORMS)}")
+    dtype, (M, Hq, d) = Q.dtype, Q.shape
+    q = _strided(Q, "Q", Q.shape, dtype, index)
+    Hk, k = 0, (None, 0, 0)
+    if K is not None:
+        if K.dim() != 3:
+            raise ValueError("K must have three dimensions")
+        Hk = K.shape[1]
+        k = _strided(K, "K", (M, Hk, d), dtype, index)
+    elif wk is not None:
+        raise ValueError("wk needs K")
+    rot = far = 0
+    tp = pp = None
+    if (table is None) != (positions is None):
+        raise ValueError("table and positions need each other")
+    if table is not None:
+        if table.dim() != 2 or table.shape[1] > d or table.shape[1] % 2:
+            raise ValueError(f"table must have two dimensions, and an even number of columns up to {d}")
+        far, rot = table.shape
+        tp, pp = _dense(table, "table", (far, rot), _F32, index), _dense(positions, "positions", (M,), _I32, index)
+    return dt, index, M, Hq, Hk, d, rot, q, k, (_dense(wq, "wq", (d,), dtype, index), _dense(wk, "wk", (d,), dtype, index), tp, far, pp)
+
+
+@_on_stream
+def head_norm_fwd(Q, K=None, wq=None, wk=None, table=None, positions=None, *, norm: str = "rms", eps, q_scale: float = 1.0,
+                  pairs: bool = False):
+    """Norm of every head of Q [M, Hq, d] and K [M, Hk, d] or None (float32 or bfloat16, tokens and heads may lie apart), "rms" or "l2",
+    with weights wq, wk [d] or None, and the rotation by positions [M] (int32) of the table's columns (rotary_table; None: no rotation),
+    in halves or in neighbouring pairs (pf_head_norm_fwd).  Returns (Yq, Yk), dense; Yq is times q_scale, Yk None without K."""
+    dt, index, M, Hq, Hk, d, rot, q, k, rest = _heads_of(Q, K, wq, wk, table, positions, norm)
+    Yq = _empty((M, Hq, d), dtype=Q.dtype, device=Q.device)
+    Yk = None if K is None else _empty((M, Hk, d), dtype=Q.dtype, device=Q.device)
+    _call(_lib.pf_head_norm_fwd, "pf_head_norm_fwd", index, *q, *k, *rest, Yq.data_ptr(), None if Yk is None else Yk.data_ptr(), M, Hq, Hk, d,
+          rot, NORMS[norm], bool(pairs), eps, q_scale, dt)
+    return Yq, Yk
+
+
+@_on_stream
+def head_norm_bwd(Q, K, dYq, dYk, wq=None, wk=None, table=None, positions=None, *, norm: str = "rms", eps, q_scale: float = 1.0,
+                  pairs: bool = False, workspace=None):
+    """Backward of head_norm_fwd from what it was given and the gradients of what it returned (K and dYk may be None).  Returns
+    (dQ, dK, dwq, dwk): dQ, dK dense in the inputs' type (dK None without K), dwq, dwk in float32, each None without its weight."""
+    dt, index, M, Hq, Hk, d, rot, q, k, rest = _heads_of(Q, K, wq, wk, table, positions, norm)
+    dtype, device = Q.dtype, Q.device
+    if (K is None) != (dYk is None):
+        raise ValueError("K and dYk need each other")
+    yq = _strided(dYq, "dYq", (M, Hq, d), dtype, index)
+    yk = (None, 0, 0) if K is None else _strided(dYk, "dYk", (M, Hk, d), dtype, index)
+    dQ = _empty((M, Hq, d), dtype=dtype, device=device)
+    dK = None if K is None else _empty((M, Hk, d), dtype=dtype, device=device)
+    dwq, dwk = (None if w is None else _empty(d, dtype=_F32, device=device) for w in (wq, wk))
+    keep = kp = None
+    kb = 0
+    if wq is not None or wk is not None:
+        keep, kp, kb = _workspace(_lib.pf_head_norm_bwd_workspace_bytes(M, Hq, Hk, d, rot) if workspace is None else 0, workspace, device)
+    at = [None if t is None else t.data_ptr() for t in (dQ, dK, dwq, dwk)]
+    _call(_lib.pf_head_norm_bwd, "pf_head_norm_bwd", index, *q, *k, *yq, *yk, *rest, *at, M, Hq, Hk, d, rot, NORMS[norm], bool(pairs), eps,
+          q_scale, dt, kp, kb)
+    return dQ, dK, dwq, dwk
+
+
+def _gated_delta_of(Q, K, V, G, beta, S0, offsets):
+    """What gated_delta_fwd and gated_delta_bwd check alike: type code, device index, sizes and the arguments from Q on."""
+    dt, index = _first(Q, "Q", 4)
+    dtype = Q.dtype
+    B, L, Hk, dk = Q.shape
+    if V.dim() != 4:
+        raise ValueError("V must have four dimensions")
+    Hv, dv = V.shape[2:]
+    if Hk == 0 or Hv % Hk:
+        raise ValueError("the heads of V must be a multiple of those of Q")
+    arrays = (*_strided(Q, "Q", Q.shape, dtype, index), *_strided(K, "K", Q.shape, dtype, index),
+              *_strided(V, "V", (B, L, Hv, dv), dtype, index), *_free(G, "G", (B, L, Hv), dtype, index),
+              *_free(beta, "beta", (B, L, Hv), dtype, index))
+    N, op = B, None
+    if offsets is not None:
+        if B != 1 or offsets.dim() != 1 or offsets.shape[0] < 1:
+            raise ValueError("packed sequences are one row of tokens, with offsets of one dimension, one more than there are sequences")
+        N = offsets.shape[0] - 1
+        op = _dense(offsets, "offsets", offsets.shape, _I32, index)
+    return dt, index, (N, L, Hk, Hv, dk, dv), arrays, _dense(S0, "S0", (N, Hv, dv, dk), _F32, index), op
+
+
+@_on_stream
+def gated_delta_fwd(Q, K, V, G, beta, S0=None, *, offsets=None, workspace=None):
+    """The gated delta rule S_t = exp(g_t) S_{t-1} (I - beta_t k_t k_t^T) + beta_t v_t k_t^T, o_t = S_t q_t (pf_gated_delta_fwd).
+    Q, K [B, L, Hk, dk], V [B, L, Hv, dv], G, beta [B, L, Hv] (float32 or bfloat16, in any order of the outer dimensions), S0 [B, Hv, dv,
+    dk] float32 or None.  Hv / Hk heads of values share a head of queries and keys.  With offsets [N + 1] (int32, on the device) B is 1 and
+    sequence n is rows offsets[n] .. offsets[n + 1] - 1, S0 [N, Hv, dv, dk]; O's rows of no sequence are not written.
+    Returns (O [B, L, Hv, dv], S_L like S0)."""
+    dt, index, sizes, arrays, sp, op = _gated_delta_of(Q, K, V, G, beta, S0, offsets)
+    N, L, Hk, Hv, dk, dv = sizes
+    device = Q.device
+    O, SL = _empty(V.shape, dtype=Q.dtype, device=device), _empty((N, Hv, dv, dk), dtype=_F32, device=device)
+    keep, kp, kb = _workspace(_lib.pf_gated_delta_workspace_bytes(*sizes, op is not None, 0, dt) if workspace is None else 0, workspace, device)
+    _call(_lib.pf_gated_delta_fwd, "pf_gated_delta_fwd", index, *arrays, sp, op, O.data_ptr(), SL.data_ptr(), *sizes, dt, kp, kb)
+    return O, SL
+
+
+@_on_stream
+def gated_delta_bwd(Q, K, V, G, beta, dO, S0=None, dSL=None, *, offsets=None, workspace=None):
+    """Backward of gated_delta_fwd (pf_gated_delta_bwd) from its inputs, dO the gradient of O (in any order of the outer dimensions)
+    and dSL that of S_L (float32, None: none).  Returns (dQ, dK, dV, dG, dbeta, dS0), all dense; rows of no sequence are not written."""
+    dt, index, sizes, arrays, sp, op = _gated_delta_of(Q, K, V, G, beta, S0, offsets)
+    N, L, Hk, Hv, dk, dv = sizes
+    dtype, device = Q.dtype, Q.device
+    o = _strided(dO, "dO", V.shape, dtype, index)
+    ep = _dense(dSL, "dSL", (N, Hv, dv, dk), _F32, index)
+    dQ, dK, dV, dG, db = (_empty(t.shape, dtype=dtype, device=device) for t in (Q, K, V, G, beta))
+    dS0 = _empty((N, Hv, dv, dk), dtype=_F32, device=device)
+    keep, kp, kb = _workspace(_lib.pf_gated_delta_workspace_bytes(*sizes, op is not None, 1, dt) if workspace is None else 0, workspace, device)
+    _call(_lib.pf_gated_delta_bwd, "pf_gated_delta_bwd", index, *arrays, *o, sp, ep, op, dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), dG.data_ptr(),
+          db.data_ptr(), dS0.data_ptr(), *sizes, dt, kp, kb)
+    return dQ, dK, dV, dG, db, dS0
+
+
+@_on_stream
+def gated_delta_step(Q, K, V, G, beta, S, slots=None):
+    """One token of the gated delta rule for B sequences (pf_gated_delta_step): Q, K [B, Hk, dk], V [B, Hv, dv], G, beta [B, Hv]
+    (float32 or bfloat16), S [pool, Hv, dv, dk] float32 the pool of states, changed in place, slots [B] int32 the state of each sequence (None: the
+    b-th; one that is not in the pool, as -1, or that a sequence before has: none, o is zero).  Returns O [B, Hv, dv]."""
+    dt, index = _first(Q, "Q", 3)
+    dtype = Q.dtype
+    B, Hk, dk = Q.shape
+    if V.dim() != 3 or S.dim() != 4:
+        raise ValueError("V must have three dimensions and S four")
+    Hv, dv = V.shape[1:]
+    if Hk == 0 or Hv % Hk:
+        raise ValueError("the heads of V must be a multiple of those of Q")
+    arrays = (*_strided(Q, "Q", Q.shape, dtype, index), *_strided(K, "K", Q.shape, dtype, index),
+              *_strided(V, "V", (B, Hv, dv), dtype, index), *_free(G, "G", (B, Hv), dtype, index), *_free(beta, "beta", (B, Hv), dtype, index))
+    pool = S.shape[0]
+    if slots is None and pool < B:
+        raise ValueError(f"S must hold {B} states at least")
+    sp, np = _dense(S, "S", (pool, Hv, dv, dk), _F32, index), _dense(slots, "slots", (B,), _I32, index)
+    O = _empty((B, Hv, dv), dtype=dtype, device=Q.device)
+    _call(_lib.pf_gated_delta_step, "pf_gated_delta_step", index, *arrays, sp, np, O.data_ptr(), B, pool, Hk, Hv, dk, dv, dt)
+    return O
