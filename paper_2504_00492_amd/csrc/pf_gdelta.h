@@ -8,10 +8,11 @@
 //   T = (I + A)^-1 ,  A_ij = beta_i D_ij k_i.k_j (j < i) ,  P_ij = D_ij q_i.k_j (j <= i)      each chunk by itself: the flow kernel
 //   U = T beta (V - gamma K S^T) ,  O = gamma Q S^T + P U ,  S' = gamma_64 S + (delta U)^T K  chunk after chunk: the scan kernel
 //
-// Numbers.  The state and everything that it is made from are held in fp32 and multiplied as such: fp32 operands take the fp32 matrix
-// instruction; where an operand is an input in bf16, the other is split into bf16 numbers whose sum it is, three of them
-// (24 bits) on the way into a state, two (16 bits) on the way into an output that is rounded to bf16.  Three bf16 instructions of
-// 32 steps take 3/4 of the time of the eight fp32 ones.
+// Numbers.  The state and everything that it is made from are held in fp32 and multiplied as such.  An fp32 matrix instruction does 64
+// operations a cycle, the bf16 one 1024, so numbers are split into bf16 ones whose sum they are: three of them (24 bits) on the way into a
+// state, two (16 bits) on the way into an output that is rounded to bf16.  An input in bf16 is one part by itself: three products of
+// 32 steps take 48 cycles where the fp32 instructions take 256; of three parts times three the six products down to 2^-24, 96
+// cycles.  Inputs in fp32 take the fp32 instruction.
 #pragma once
 #include "pf_layer_common.h"
 #include "pf_layer_internal.h"
@@ -74,17 +75,49 @@ template <typename T> __device__ __forceinline__ f32x4 mma22(const Of<T, 2> &a, 
     }
 }
 
+// three parts each: what is left out is 2^-24 of the whole
+__device__ __forceinline__ f32x4 mma33(const Of<bf16, 3> &a, const Of<bf16, 3> &b, f32x4 c)
+{
+    c = mfma16(a.p[2], b.p[0], c);
+    c = mfma16(a.p[1], b.p[1], c);
+    c = mfma16(a.p[0], b.p[2], c);
+    c = mfma16(a.p[1], b.p[0], c);
+    c = mfma16(a.p[0], b.p[1], c);
+    return mfma16(a.p[0], b.p[0], c);
+}
+template <int NP> __device__ __forceinline__ f32x4 mma_parts(const Of<bf16, NP> &a, const Of<bf16, NP> &b, f32x4 c)
+{
+    if constexpr (NP == 2) return mma22<bf16>(a, b, c);
+    else return mma33(a, b, c);
+}
+
 template <int N> struct F32s;
 template <> struct F32s<4> { typedef f32x4 f; typedef bf16x4 b; };
 template <> struct F32s<8> { typedef f32x8 f; typedef bf16x8 b; };
-// x as a sum of NP bf16 numbers, each the rest rounded to nearest even
+// x as a sum of NP bf16 numbers, each the rest rounded to nearest even (two at a time: a pair of conversions is one instruction)
 template <int NP, int N> __device__ __forceinline__ void split(typename F32s<N>::f x, typename F32s<N>::b (&p)[NP])
 {
+    uint32_t r[NP][N / 2];
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        p[i] = __builtin_convertvector(x, typename F32s<N>::b);
-        if (i + 1 < NP) x -= __builtin_convertvector(p[i], typename F32s<N>::f);
+    for (int j = 0; j < N / 2; ++j) {
+        f32x2 v = {x[2 * j], x[2 * j + 1]};
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const uint32_t u = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+            r[i][j] = u;
+            if (i + 1 < NP) v[0] -= __uint_as_float(u << 16), v[1] -= __uint_as_float(u & 0xffff0000u);
+        }
     }
+#pragma unroll
+    for (int i = 0; i < NP; ++i) __builtin_memcpy(&p[i], r[i], sizeof(p[i]));
+}
+// parts times an input; one in fp32 is split as well
+__device__ __forceinline__ f32x4 mma_input(const Of<bf16, 3> &a, In<bf16> b, f32x4 c) { return mma<3>(a, b, c); }
+__device__ __forceinline__ f32x4 mma_input(const Of<bf16, 3> &a, In<float> b, f32x4 c)
+{
+    Of<bf16, 3> p;
+    split<3, 8>(b.v, p.p);
+    return mma33(a, p, c);
 }
 template <typename T, int NP> __device__ __forceinline__ Of<T, NP> of(f32x8 x)
 {
@@ -120,6 +153,21 @@ template <typename T> __device__ __forceinline__ In<T> frag_cols(const T *tile, 
     return r;
 }
 
+// the same, but the 16 lanes have the columns n + 8 (r16 / 4) + 4 half + r16 % 4: of two such fragments' results, half = 0 and 1, a lane
+// has the eight neighbours n + 8 g ..
+template <typename T> __device__ __forceinline__ In<T> frag_cols8(const T *tile, int ld, int k, int n, int half, int r16)
+{
+    In<T> r;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r.v[e] = tile[(k + e) * ld + n + 8 * (r16 >> 2) + 4 * half + (r16 & 3)];
+    } else {
+        const T *p = tile + (k + (r16 >> 2)) * ld + n + 8 * (r16 & 3) + 4 * half;
+        r.v = join(lds_read_tr4(p), lds_read_tr4(p + 4 * ld));
+    }
+    return r;
+}
+
 // Computed numbers, R rows of K: NP planes of bf16, or fp32.
 template <typename T, int NP, int R, int K> struct Tile {
     static constexpr int kLd = pitch<T>(K), kPlane = R * kLd, kBytes = (sizeof(T) == 4 ? 1 : NP) * kPlane * (int)sizeof(T);
@@ -133,6 +181,18 @@ template <typename T, int NP, int R, int K> struct Tile {
             split<NP, 4>(x, p);
 #pragma unroll
             for (int i = 0; i < NP; ++i) *reinterpret_cast<bf16x4 *>(at + i * kPlane + row * kLd + k) = p[i];
+        }
+    }
+    // the first parts of eight neighbours
+    template <int PARTS> __device__ __forceinline__ void put8(int row, int k, const Of<T, PARTS> &x) const
+    {
+        static_assert(NP <= PARTS);
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<f32x4 *>(at + row * kLd + k) = __builtin_shufflevector(x.v, x.v, 0, 1, 2, 3);
+            *reinterpret_cast<f32x4 *>(at + row * kLd + k + 4) = __builtin_shufflevector(x.v, x.v, 4, 5, 6, 7);
+        } else {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) st8(at + i * kPlane + row * kLd + k, x.p[i]);
         }
     }
     __device__ __forceinline__ Of<T, NP> rows(int row, int k) const
@@ -204,23 +264,35 @@ __device__ __forceinline__ Sequence sequence_at(const GDelta &a, int seq)
 // row of the dense outputs [.., tokens, H, d]
 __device__ __forceinline__ long long out_row(const GDelta &a, int seq, int tok) { return (long long)seq * a.rows + tok; }
 
-// ---- what the flow kernel leaves for each chunk and value head: T and P [64][64] (blocks of 16 above the diagonal are not
-// written, but the upper right of each two are zeros), and of each token: gamma, delta, beta, and G in units of log 2 as a double
-constexpr int kMatrix = C * C, kVec = 5 * C;
+// ---- what the flow kernel leaves for each chunk and value head.  Matrices of pairs of tokens, as three bf16 numbers each (24 bits): T and
+// P (of P as many as the forward uses), for the backward T and the transposes of both.  They are kept as the fragments that the
+// scans take, 16 rows by 32 columns, each part of one 1 KB as its 64 lanes hold it, and of the triangle only: rows 16 w .. have the
+// columns up to theirs (transposed: from theirs on), six fragments.
+constexpr int kMatrix = 6 * 3 * 512;
+__host__ __device__ constexpr int low_fragment(int w, int t) { return w < 2 ? w : 2 * w - 2 + t; }
+__host__ __device__ constexpr int high_fragment(int w, int t) { return w < 2 ? 2 * w + t : w + 2; }
+// and of each token: gamma, delta, beta, and G in units of log 2 as two numbers, a multiple of 1/16 and the rest, so that differences
+// of far sums keep their last bits
+constexpr int kVec = 5 * C;
 struct Vec {
-    const float *gamma, *delta, *beta;
-    const double *G;
+    const float *gamma, *delta, *beta, *coarse, *fine;
 };
 __device__ __forceinline__ Vec vec_at(const float *vec, long long x)
 {
     const float *p = vec + x * kVec;
-    return {p, p + C, p + 2 * C, reinterpret_cast<const double *>(p + 3 * C)};
+    return {p, p + C, p + 2 * C, p + 3 * C, p + 4 * C};
 }
-// 2^x to fp32's accuracy wherever x lies
+// 2^(coarse + fine), coarse a multiple of 1/16
+__device__ __forceinline__ float power(float coarse, float fine)
+{
+    const float n = __builtin_rintf(coarse);
+    return __builtin_ldexpf(__builtin_amdgcn_exp2f((coarse - n) + fine), (int)n);
+}
+__device__ __forceinline__ float coarse_of(double x) { return (float)(__builtin_rint(x * 16.) * 0.0625); }
 __device__ __forceinline__ float power(double x)
 {
-    const double n = __builtin_rint(x);
-    return __builtin_ldexpf(__builtin_amdgcn_exp2f((float)(x - n)), (int)n);
+    const float coarse = coarse_of(x);
+    return power(coarse, (float)(x - coarse));
 }
 
 // The log of a gate as it is used: exp(-256) and exp(256) are 0 and infinite in fp32, also times what else it holds beside them here.

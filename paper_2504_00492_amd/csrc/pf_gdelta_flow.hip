@@ -62,17 +62,37 @@ __global__ __launch_bounds__(1024) void plan_kernel(GDelta a)
     }
 }
 
+// A matrix in LDS (TURNED: its transpose) as fragments in NP bf16 parts.
+template <int NP, bool TURNED> __device__ __forceinline__ void put_matrix(const float *tile, int ld, bf16 *to)
+{
+#pragma unroll
+    for (int u0 = 0; u0 < 384; u0 += 256) {
+        const int u = u0 + threadIdx.x, f = u >> 6, lane = u & 63;
+        if (u >= 384) break;
+        const int w = TURNED ? (f < 4 ? f >> 1 : f - 2) : f < 2 ? f : (f + 2) >> 1, t = TURNED ? (f < 4 ? f & 1 : 1) : f < 2 ? 0 : f & 1;
+        const int row = 16 * w + (lane & 15), col = 32 * t + 8 * (lane >> 4);
+        f32x8 v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = TURNED ? tile[(col + e) * ld + row] : tile[row * ld + col + e];
+        bf16x8 p[NP];
+        split<NP, 8>(v, p);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) st8(to + ((f * 3 + i) * 64 + lane) * 8, p[i]);
+    }
+}
+
 // One workgroup of four wavefronts for each chunk and value head; wavefront w has the rows 16 w ..  What it cannot do without is
 // reading K and Q (32 KB at d_k = 128 in bf16) and writing T and P.
-template <typename T, int DK, bool FULL>
+template <typename T, int DK, bool FULL, bool BACKWARD>
 __global__ __launch_bounds__(256) void flow_kernel(GDelta a)
 {
-    constexpr int KP = pitch<T>(DK), AP = C + 4, KS = DK / 32;
-    __shared__ __attribute__((aligned(16))) T Ks[C * KP];
+    constexpr int KP = pitch<T>(DK), AP = C + 4, KS = DK / 32, kTokens = C * KP * (int)sizeof(T), kTile = C * AP * 4;
+    __shared__ __attribute__((aligned(16))) char smem[kTokens > kTile ? kTokens : kTile];
     __shared__ __attribute__((aligned(16))) float A[C * AP];
     __shared__ __attribute__((aligned(16))) float diag[C * 20];
-    __shared__ double sG[C];
-    __shared__ float sbeta[C];
+    __shared__ float coarse[C], fine[C], sbeta[C];
+    T *Ks = reinterpret_cast<T *>(smem);
+    float *P = reinterpret_cast<float *>(smem);      // in K's place
 
     const int id = (int)xcd_consecutive(blockIdx.x, gridDim.x), chunk = id / a.Hv, h = id - chunk * a.Hv, hk = h / (a.Hv / a.Hk);
     Chunk x;
@@ -105,13 +125,14 @@ __global__ __launch_bounds__(256) void flow_kernel(GDelta a)
             if (lane >= s) G += other;
         }
         const double whole = __shfl(G, 63);
-        sG[lane] = G;
-        sbeta[lane] = beta;
+        const float c = coarse_of(G), f = (float)(G - c);
+        coarse[lane] = c, fine[lane] = f, sbeta[lane] = beta;
         float *v = a.vec + xi * kVec;
         v[lane] = power(G);
         v[C + lane] = power(whole - G);
         v[2 * C + lane] = beta;
-        reinterpret_cast<double *>(v + 3 * C)[lane] = G;
+        v[3 * C + lane] = c;
+        v[4 * C + lane] = f;
     }
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) {
@@ -134,22 +155,22 @@ __global__ __launch_bounds__(256) void flow_kernel(GDelta a)
             qk[ct] = mma(qf[s], kb, qk[ct]);
         }
     }
-    float *P = a.P + xi * kMatrix, *To = a.T + xi * kMatrix;
+    __syncthreads();
 #pragma unroll
     for (int ct = 0; ct < 4; ++ct) {
         const int j = 16 * ct + r16;
         if (ct <= w) {
-            const double Gj = sG[j];
+            const float cj = coarse[j], fj = fine[j];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int i = 16 * w + 4 * g + e;
-                const float D = power(sG[i] - Gj);
+                const float D = power(coarse[i] - cj, fine[i] - fj);
                 A[i * AP + j] = j < i ? sbeta[i] * (D * kk[ct][e]) : 0.f;
-                P[i * C + j] = j <= i ? D * qk[ct][e] : 0.f;
+                P[i * AP + j] = j <= i ? D * qk[ct][e] : 0.f;
             }
         } else if (ct == w + 1 && (w & 1) == 0) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) P[(16 * w + 4 * g + e) * C + j] = 0.f;
+            for (int e = 0; e < 4; ++e) P[(16 * w + 4 * g + e) * AP + j] = 0.f;
         }
     }
     __syncthreads();
@@ -173,14 +194,13 @@ __global__ __launch_bounds__(256) void flow_kernel(GDelta a)
     for (int e = 0; e < 4; ++e) {
         own[e] = g == 0 ? v[e] : g == 1 ? v[4 + e] : g == 2 ? v[8 + e] : v[12 + e];
         diag[(16 * w + 4 * g + e) * 20 + r16] = own[e];
-        To[(16 * w + 4 * g + e) * C + 16 * w + r16] = own[e];
     }
     __syncthreads();
     // below the diagonal, a column of blocks to a wavefront: T_ij = -T_ii sum over k of A_ik T_kj; a tile that was computed is the next
     // product's right operand as it stands
+    f32x4 t[4];
     auto column = [&](auto col) {
         constexpr int J = decltype(col)::value;
-        f32x4 t[4];
         t[J] = own;
 #pragma unroll
         for (int i = J + 1; i < 4; ++i) {
@@ -188,19 +208,35 @@ __global__ __launch_bounds__(256) void flow_kernel(GDelta a)
 #pragma unroll
             for (int k = J; k < i; ++k) X = mma4(*reinterpret_cast<const f32x4 *>(&A[(16 * i + r16) * AP + 16 * k + 4 * g]), t[k], X);
             t[i] = -mma4(*reinterpret_cast<const f32x4 *>(&diag[(16 * i + r16) * 20 + 4 * g]), X, zero4());
-#pragma unroll
-            for (int e = 0; e < 4; ++e) To[(16 * i + 4 * g + e) * C + 16 * J + r16] = t[i][e];
         }
     };
     if (w == 0) column(std::integral_constant<int, 0>{});
     else if (w == 1) column(std::integral_constant<int, 1>{});
     else if (w == 2) column(std::integral_constant<int, 2>{});
+    else column(std::integral_constant<int, 3>{});
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (i < w && !(i == w - 1 && (w & 1))) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) A[(16 * i + 4 * g + e) * AP + 16 * w + r16] = i < w ? 0.f : t[i][e];
+    }
+    __syncthreads();
+    put_matrix<3, false>(A, AP, a.T + xi * kMatrix);
+    if constexpr (BACKWARD) {
+        put_matrix<3, true>(A, AP, a.Tt + xi * kMatrix);
+        put_matrix<3, true>(P, AP, a.P + xi * kMatrix);
+    } else {
+        put_matrix<sizeof(T) == 2 ? 2 : 3, false>(P, AP, a.P + xi * kMatrix);
+    }
 }
 
 template <typename T, int DK> hipError_t flow(const GDelta &a, hipStream_t stream)
 {
     const dim3 grid((unsigned)((long long)a.chunks * a.Hv));
-    gdelta_full(a, sizeof(T)) ? flow_kernel<T, DK, true><<<grid, 256, 0, stream>>>(a) : flow_kernel<T, DK, false><<<grid, 256, 0, stream>>>(a);
+    const bool full = gdelta_full(a, sizeof(T));
+    if (a.Tt) full ? flow_kernel<T, DK, true, true><<<grid, 256, 0, stream>>>(a) : flow_kernel<T, DK, false, true><<<grid, 256, 0, stream>>>(a);
+    else full ? flow_kernel<T, DK, true, false><<<grid, 256, 0, stream>>>(a) : flow_kernel<T, DK, false, false><<<grid, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 template <typename T> hipError_t flow(const GDelta &a, hipStream_t stream)
@@ -224,6 +260,7 @@ size_t gdelta_workspace(GDelta &a, bool backward, void *at)
     part(a.T, x * gd::kMatrix);
     part(a.P, x * gd::kMatrix);
     if (backward) {
+        part(a.Tt, x * gd::kMatrix);
         part(a.S, x * gdelta_state(a));
         part(a.R, x * gdelta_state(a));
         part(a.U, x * gd::C * dv);

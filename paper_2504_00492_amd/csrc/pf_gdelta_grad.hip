@@ -26,7 +26,7 @@ __global__ __launch_bounds__(256) void grad_kernel(GDelta a)
     constexpr int kStates = 2 * StateTile::kBytes, kTokens = C * KP * (int)sizeof(T);
     static_assert(UTile::kBytes <= kStates, "U comes in the place of S and R");
     __shared__ __attribute__((aligned(16))) char smem[kStates + 2 * kTokens + 2 * PairTile::kBytes];
-    __shared__ double sG[C];
+    __shared__ float coarse[C], fine[C];
     __shared__ float srow[C], scol[4][C], sdot[4];
     const StateTile Ss = {reinterpret_cast<T *>(smem)}, Rs = {reinterpret_cast<T *>(smem + StateTile::kBytes)};
     const UTile Us = {reinterpret_cast<T *>(smem)};
@@ -52,7 +52,7 @@ __global__ __launch_bounds__(256) void grad_kernel(GDelta a)
     // eight values of d_v of the lane's token: rows behind the end count as zeros
     auto o_at = [&](int v) { return fetch<T, false>(dO + v, 16 * w + r16 < x.len ? a.dv - v : 0); };
 
-    if (threadIdx.x < C) sG[threadIdx.x] = vec.G[threadIdx.x];
+    if (threadIdx.x < C) coarse[threadIdx.x] = vec.coarse[threadIdx.x], fine[threadIdx.x] = vec.fine[threadIdx.x];
     const f32x4 gamma = *reinterpret_cast<const f32x4 *>(vec.gamma + i0), delta = *reinterpret_cast<const f32x4 *>(vec.delta + i0);
     const f32x4 beta = *reinterpret_cast<const f32x4 *>(vec.beta + i0);
 
@@ -87,7 +87,7 @@ __global__ __launch_bounds__(256) void grad_kernel(GDelta a)
 #pragma unroll
         for (int n = 0; n < 4; ++n) kk[n] = mma(ka, fetch<T, FULL>(K + min(16 * n + r16, x.len - 1) * a.kt + k, a.dk - k), kk[n]);
     }
-    const float *P = a.P + xi * kMatrix;
+    const bf16 *Pt = a.P + xi * kMatrix;      // of the transpose, in three parts
     f32x4 row = zero4(), yk = zero4();
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
@@ -95,17 +95,21 @@ __global__ __launch_bounds__(256) void grad_kernel(GDelta a)
         f32x4 w1 = zero4(), w2 = zero4();
         float col = 0.f;
         if (n <= w) {
-            const double Gj = sG[j];
+            const float cj = coarse[j], fj = fine[j];
+            f32x4 p = zero4();
+#pragma unroll
+            for (int q = 2; q >= 0; --q)
+                p += __builtin_convertvector(ld4(Pt + ((high_fragment(n, w >> 1) * 3 + q) * 64 + r16 + 16 * (2 * (w & 1) + (g >> 1))) * 8 + 4 * (g & 1)), f32x4);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int i = i0 + e;
-                const float D = power(sG[i] - Gj), p = P[i * C + j];
+                const float D = power(coarse[i] - cj, fine[i] - fj);
                 const bool in = i < x.len;
                 w1[e] = in && j <= i ? D * X[n][e] : 0.f;
                 const float y = in && j < i ? -Y[n][e] * D : 0.f;
                 w2[e] = beta[e] * y;
                 yk[e] += y * kk[n][e];
-                const float both = (in && j < i ? X[n][e] * p : 0.f) + w2[e] * kk[n][e];
+                const float both = (in && j < i ? X[n][e] * p[e] : 0.f) + w2[e] * kk[n][e];
                 row[e] += both;
                 col += both;
             }

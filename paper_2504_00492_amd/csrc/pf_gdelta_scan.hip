@@ -1,12 +1,16 @@
-// Gated delta rule: the chains over the chunks of a sequence (pf_gdelta.h), forward and backward.  A workgroup of four wavefronts
-// has 16 NT rows of a state, [d_v][d_k], for one sequence and value head; its rows are in registers as accumulator tiles of the
-// transposed state, tiles of 16 of d_k shared out among the wavefronts, and of everything that runs along the tokens of a chunk a
-// wavefront has the 16 tokens 16 w ..
+// Gated delta rule: the chains over the chunks of a sequence (pf_gdelta.h), forward and backward.  A workgroup has 16 rows of a state,
+// [d_v][d_k], for one sequence and value head.  A chunk's steps come one from the other, and what bounds these kernels is how long they take
+// (0.8 us where the arithmetic alone takes half), so eight wavefronts share the work by what waits for what: four have
+// the chain alone, with the state in registers as accumulator tiles of its transpose (tiles of 16 of d_k shared out among them;
+// of what runs along the tokens a wavefront has the 16 tokens 16 w ..), and four beside them do all that does not lie in it: they bring
+// K into LDS a chunk ahead, and compute the outputs, or in the backward what R does not enter.
 #include "pf_gdelta.h"
 
 namespace pf {
 namespace gd {
 namespace {
+
+constexpr int N = 16;      // rows of a state to a workgroup
 
 // four values of a state's row from k on
 template <bool FULL> __device__ __forceinline__ f32x4 state4(const float *row, int k, int dk)
@@ -32,445 +36,516 @@ template <bool FULL> __device__ __forceinline__ void state4(float *row, int k, i
     }
 }
 
-// K or Q of a chunk on its way into LDS
-template <typename T, int DK, bool FULL> struct Staged {
-    static constexpr int UNITS = C * DK / 8 / 256;
+// K or Q of a chunk.  LDS: by way of it (256 threads bring it there); else, where that has no room, out of memory each time.
+template <typename T, int DK, bool FULL, bool LDS> struct Tokens {
+    static constexpr int kLd = pitch<T>(DK), kBytes = LDS ? C * kLd * (int)sizeof(T) : 0, UNITS = LDS ? C * DK / 8 / 256 : 1;
     In<T> r[UNITS];
-    __device__ __forceinline__ void load(const T *p, long long step, int len, int dk)
+    __device__ __forceinline__ void load(const T *p, long long step, int len, int dk, int thread)
     {
+        if constexpr (LDS) {
 #pragma unroll
-        for (int i = 0; i < UNITS; ++i) {
-            const int u = i * 256 + threadIdx.x, row = u / (DK / 8), k = 8 * (u % (DK / 8));
-            r[i] = fetch<T, FULL>(p + min(row, len - 1) * step + k, dk - k);
+            for (int i = 0; i < UNITS; ++i) {
+                const int u = i * 256 + thread, row = u / (DK / 8), k = 8 * (u % (DK / 8));
+                r[i] = fetch<T, FULL>(p + min(row, len - 1) * step + k, dk - k);
+            }
         }
     }
-    __device__ __forceinline__ void store(T *tile) const
+    __device__ __forceinline__ void store(T *tile, int thread) const
     {
+        if constexpr (LDS) {
 #pragma unroll
-        for (int i = 0; i < UNITS; ++i) {
-            const int u = i * 256 + threadIdx.x;
-            __builtin_memcpy(__builtin_assume_aligned(tile + u / (DK / 8) * pitch<T>(DK) + 8 * (u % (DK / 8)), 16), &r[i], sizeof(r[i]));
+            for (int i = 0; i < UNITS; ++i) {
+                const int u = i * 256 + thread;
+                __builtin_memcpy(__builtin_assume_aligned(tile + u / (DK / 8) * kLd + 8 * (u % (DK / 8)), 16), &r[i], sizeof(r[i]));
+            }
+        }
+    }
+    static __device__ __forceinline__ In<T> rows(const T *tile, const T *p, long long step, int len, int dk, int row, int k)
+    {
+        if constexpr (LDS) return frag_rows(tile, kLd, row, k);
+        else return fetch<T, FULL>(p + min(row, len - 1) * step + k, dk - k);
+    }
+    static __device__ __forceinline__ In<T> cols8(const T *tile, const T *p, long long step, int len, int dk, int k, int n, int half, int r16)
+    {
+        if constexpr (LDS) {
+            return frag_cols8(tile, kLd, k, n, half, r16);
+        } else {
+            In<T> f;
+            const int c = n + 8 * (r16 >> 2) + 4 * half + (r16 & 3);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f.v[e] = FULL || c < dk ? p[min(k + e, len - 1) * step + c] : (T)0.f;
+            return f;
         }
     }
 };
 
-// Forward.  OUT: O is wanted; else the states before every chunk and U are kept for the backward.
-template <typename T, int DK, int NT, bool FULL, bool OUT>
-__global__ __launch_bounds__(256) void scan_kernel(GDelta a)
+// The parts of a matrix of pairs: what rows 16 w .. have of its triangle (LOW: up to the diagonal, else from it on), `lane` the lane's place
+// in a fragment.
+template <int NP, bool LOW> struct Pairs {
+    Of<bf16, NP> f[2];
+    __device__ __forceinline__ void load(const bf16 *p, int w, int lane)
+    {
+        p += (LOW ? low_fragment(w, 0) : high_fragment(w, w >> 1)) * 3 * 512 + lane * 8;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) f[LOW ? 0 : 1].p[i] = ld8(p + i * 512 + (LOW ? 0 : w < 2 ? 3 * 512 : 0));
+        if (LOW ? w >= 2 : w < 2)
+#pragma unroll
+            for (int i = 0; i < NP; ++i) f[LOW ? 1 : 0].p[i] = ld8(p + i * 512 + (LOW ? 3 * 512 : 0));
+    }
+};
+
+struct Place {      // of a workgroup: its sequence, head and first row of the state
+    int seq, h, hk, dv0, chunks;
+    Sequence q;
+    long long sh;
+};
+__device__ __forceinline__ Place place_of(const GDelta &a, int tiles)
 {
-    constexpr int KP = pitch<T>(DK), KS = DK / 32, DT = DK / 64, N = 16 * NT, YP = C + 4;
-    typedef Tile<T, 3, N, DK> StateTile;
-    typedef Tile<T, 3, N, C> LaterTile;
-    typedef Tile<T, 2, N, C> UTile;
-    __shared__ __attribute__((aligned(16))) T Ks[2][C * KP];
-    __shared__ __attribute__((aligned(16))) char smem[StateTile::kBytes + LaterTile::kBytes + UTile::kBytes + N * YP * 4];
-    const StateTile Sp = {reinterpret_cast<T *>(smem)};
-    const LaterTile Ud = {reinterpret_cast<T *>(smem + StateTile::kBytes)};
-    const UTile Uo = {reinterpret_cast<T *>(smem + StateTile::kBytes + LaterTile::kBytes)};
-    float *Yt = reinterpret_cast<float *>(smem + StateTile::kBytes + LaterTile::kBytes + UTile::kBytes);
-
     // tiles of one head side by side, on one XCD: they read the same K, Q, T and P
-    const int tiles = OUT ? (a.dv + N - 1) / N : (a.dv + 31) / 32 * (32 / N);
-    const int id = (int)xcd_consecutive(blockIdx.x, gridDim.x), tile = id % tiles, sh = id / tiles;
-    const int seq = sh / a.Hv, h = sh - seq * a.Hv, hk = h / (a.Hv / a.Hk), dv0 = tile * N;
-    const Sequence q = sequence_at(a, seq);
-    const int chunks = (q.len + C - 1) / C;
-    const int w = wave_id(), lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4;
+    Place x;
+    const int id = (int)xcd_consecutive(blockIdx.x, gridDim.x), sh = id / tiles;
+    x.sh = sh;
+    x.seq = sh / a.Hv, x.h = sh - x.seq * a.Hv, x.hk = x.h / (a.Hv / a.Hk), x.dv0 = (id - sh * tiles) * N;
+    x.q = sequence_at(a, x.seq);
+    x.chunks = (x.q.len + C - 1) / C;
+    return x;
+}
+__device__ __forceinline__ int wide_of(const GDelta &a) { return (a.dv + 31) / 32 * 32; }
 
-    int col[NT];      // this lane's rows of the state; those behind d_v are zeros
-    bool there[NT];
+// What a wavefront of the chain has of the state: SLABS times 32 of d_k, from 32 SLABS w on (d_k = 64: two of the four have any), as it
+// comes out of the products with the tokens and goes into the next: a lane has the eight neighbours 8 g .. of its row.
+template <int DK> struct Share {
+    static constexpr int SLABS = DK <= 128 ? 1 : DK / 128, HOLDERS = DK / 32 / SLABS;
+};
+template <bool FULL, int SLABS> __device__ __forceinline__ void get_state(const float *row, int k, int dk, f32x8 (&s)[SLABS])
+{
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) col[nt] = min(dv0 + 16 * nt + r16, a.dv - 1), there[nt] = dv0 + 16 * nt + r16 < a.dv;
-
-    f32x4 s[DT][NT];
+    for (int i = 0; i < SLABS; ++i) {
+        const f32x4 a = state4<FULL>(row, k + 32 * i, dk), b = state4<FULL>(row, k + 32 * i + 4, dk);
+        s[i] = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+}
+template <bool FULL, int SLABS> __device__ __forceinline__ void put_state(float *row, int k, int dk, const f32x8 (&s)[SLABS])
+{
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
+    for (int i = 0; i < SLABS; ++i) {
+        state4<FULL>(row, k + 32 * i, dk, __builtin_shufflevector(s[i], s[i], 0, 1, 2, 3));
+        state4<FULL>(row, k + 32 * i + 4, dk, __builtin_shufflevector(s[i], s[i], 4, 5, 6, 7));
+    }
+}
+
+// Tokens times the transposed state: each holder multiplies what it has of d_k for all 64 tokens, with the tiles of 16 tokens counted
+// from its own (w ^ i), so that registers are named at compile time; the others' parts go through LDS (1 KB as the lanes hold it).
+template <typename K, typename T, int DK>
+__device__ __forceinline__ f32x4 products(const T *Kc, const T *Kg, long long step, int len, int dk, const Of<T, 3> (&sp)[Share<DK>::SLABS],
+                                          f32x4 *parts, int w, int lane)
+{
+    const int r16 = lane & 15, g = lane >> 4;
+    f32x4 m[4];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            s[dt][nt] = zero4();
-            if (a.S0 && there[nt]) s[dt][nt] = state4<FULL>(a.S0 + ((long long)sh * a.dv + col[nt]) * a.dk, 16 * (w * DT + dt) + 4 * g, a.dk);
-        }
+    for (int i = 0; i < 4; ++i) m[i] = zero4();
+    if (w < Share<DK>::HOLDERS) {
+#pragma unroll
+        for (int t = 0; t < Share<DK>::SLABS; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                m[i] = mma<3>(K::rows(Kc, Kg, step, len, dk, 16 * (w ^ i) + r16, 32 * (w * Share<DK>::SLABS + t) + 8 * g), sp[t], m[i]);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) parts[((w ^ i) * 3 + i - 1) * 64 + lane] = m[i];
+    }
+    return m[0];
+}
+template <int DK> __device__ __forceinline__ f32x4 joined(f32x4 own, const f32x4 *parts, int w, int lane)
+{
+    const f32x4 *p = parts + w * 3 * 64 + lane;
+    if constexpr (Share<DK>::HOLDERS == 4) return (own + p[0]) + (p[64] + p[128]);
+    else return w < 2 ? own + p[0] : p[64] + p[128];
+}
 
-    const T *K = static_cast<const T *>(a.K) + seq * a.kb + q.tok * a.kt + hk * a.kh;
-    const T *Q = static_cast<const T *>(a.Q) + seq * a.qb + q.tok * a.qt + hk * a.qh;
-    const T *V = static_cast<const T *>(a.V) + seq * a.vb + q.tok * a.vt + h * a.vh;
-    T *O = static_cast<T *>(a.O);
+// Forward.  OUT: O is wanted; else the states before every chunk and U are kept for the backward.
+template <typename T, int DK, bool FULL, bool OUT>
+__global__ __launch_bounds__(512) void scan_kernel(GDelta a)
+{
+    constexpr int KS = DK / 32, NPO = sizeof(T) == 2 ? 2 : 3, SLABS = Share<DK>::SLABS, UP = C + 4;      // NPO: parts on the way into O
+    typedef Tile<T, NPO, N, DK> StateTile;
+    typedef Tile<T, 3, N, C> LaterTile;
+    typedef Tile<bf16, 3, N, C> YTile;
+    constexpr int kWork = (OUT ? StateTile::kBytes : 0) + LaterTile::kBytes + YTile::kBytes + N * UP * 4 + (12 + 4) * 1024 + 4 * C * 4;
+    typedef Tokens<T, DK, FULL, 2 * C * pitch<T>(DK) * (int)sizeof(T) + kWork <= 160 * 1024> KTile;
+    __shared__ __attribute__((aligned(16))) char smem[2 * KTile::kBytes + kWork];
+    char *at = smem + 2 * KTile::kBytes;
+    auto take = [&](int bytes) { char *p = at; at += bytes; return p; };
+    f32x4 *parts = reinterpret_cast<f32x4 *>(take(12 * 1024)), *bv = reinterpret_cast<f32x4 *>(take(4 * 1024));      // bv: beta v
+    float *rate = reinterpret_cast<float *>(take(4 * C * 4));      // beta gamma, -, delta of even and odd chunks
+    const LaterTile Ud = {reinterpret_cast<T *>(take(LaterTile::kBytes))};
+    const YTile Yp = {reinterpret_cast<bf16 *>(take(YTile::kBytes))};
+    float *Uf = reinterpret_cast<float *>(take(N * UP * 4));
+    const StateTile Sp = {reinterpret_cast<T *>(at)};
+    auto k_tile = [&](int c) { return reinterpret_cast<T *>(smem + (c & 1) * KTile::kBytes); };
 
-    Staged<T, DK, FULL> kr;
-    In<T> qf[KS];
-    T vv[NT][4];
-    f32x4 tf[4], gamma, delta, beta;
-    f32x8 pf[2];
-    float decay = 0.f;
-    auto len_of = [&](int c) { return min(C, q.len - C * c); };
-    auto load_k = [&](int c) { kr.load(K + (long long)C * c * a.kt, a.kt, len_of(c), a.dk); };
-    auto load_q = [&](int c) {
-        if constexpr (OUT) {
+    const Place x = place_of(a, OUT ? (a.dv + N - 1) / N : wide_of(a) / N);
+    const int w = wave_id() & 3, lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4, i0 = 16 * w + 4 * g;
+    const int col = min(x.dv0 + r16, a.dv - 1);      // this lane's row of the state; those behind d_v are zeros
+    const bool there = x.dv0 + r16 < a.dv;
+    const T *K = static_cast<const T *>(a.K) + x.seq * a.kb + x.q.tok * a.kt + x.hk * a.kh;
+    const long long first = (long long)x.q.first * a.Hv + x.h;
+    auto len_of = [&](int c) { return min(C, x.q.len - C * c); };
+
+    if (wave_id() >= 4) {      // ---- beside the chain
+        const int thread = threadIdx.x - 256, wide = wide_of(a);
+        const T *Q = static_cast<const T *>(a.Q) + x.seq * a.qb + x.q.tok * a.qt + x.hk * a.qh;
+        const T *V = static_cast<const T *>(a.V) + x.seq * a.vb + x.q.tok * a.vt + x.h * a.vh + col;
+        T *O = static_cast<T *>(a.O) + (out_row(a, x.seq, x.q.tok) * a.Hv + x.h) * a.dv + col;
+        KTile kr;
+        In<T> qf[KS];
+        T vv[4];
+        Pairs<NPO, true> pf;
+        f32x4 gamma, beta, delta, since;
+        auto load = [&](int c) {      // what the chain takes
+            kr.load(K + (long long)C * c * a.kt, a.kt, len_of(c), a.dk, thread);
+            const T *p = V + (long long)C * c * a.vt;
+            const int len = len_of(c);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) vv[e] = p[min(i0 + e, len - 1) * a.vt];
+            const Vec v = vec_at(a.vec, first + (long long)c * a.Hv);
+            gamma = *reinterpret_cast<const f32x4 *>(v.gamma + i0);
+            delta = *reinterpret_cast<const f32x4 *>(v.delta + i0);
+            beta = *reinterpret_cast<const f32x4 *>(v.beta + i0);
+        };
+        auto store = [&](int c) {
+            kr.store(k_tile(c), thread);
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = there ? beta[e] * to_f32(vv[e]) : 0.f;
+            bv[w * 64 + lane] = v;
+            if (r16 == 0) {
+                *reinterpret_cast<f32x4 *>(rate + i0) = beta * gamma;
+                *reinterpret_cast<f32x4 *>(rate + (2 + (c & 1)) * C + i0) = delta;
+                if (w == 3 && g == 3) rate[C + (c & 1)] = gamma[3];      // of the chunk's end
+            }
+        };
+        auto load_q = [&](int c) {
             const T *p = Q + (C * c + min(16 * w + r16, len_of(c) - 1)) * a.qt;
 #pragma unroll
             for (int t = 0; t < KS; ++t) qf[t] = fetch<T, FULL>(p + 32 * t + 8 * g, a.dk - 32 * t - 8 * g);
-        }
-    };
-    auto load_v = [&](int c) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const T *p = V + (C * c + min(16 * w + 4 * g + e, len_of(c) - 1)) * a.vt;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) vv[nt][e] = p[col[nt]];
-        }
-    };
-    auto load_t = [&](int c) {
-        const float *p = a.T + ((long long)(q.first + c) * a.Hv + h) * kMatrix + (16 * w + r16) * C + 4 * g;
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-            if (b <= w) tf[b] = *reinterpret_cast<const f32x4 *>(p + 16 * b);
-    };
-    auto load_p = [&](int c) {
-        if constexpr (OUT) {
-            const float *p = a.P + ((long long)(q.first + c) * a.Hv + h) * kMatrix + (16 * w + r16) * C + 8 * g;
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-                if (b <= w / 2) pf[b] = *reinterpret_cast<const f32x8 *>(p + 32 * b);
-        }
-    };
-    auto load_vec = [&](int c) {
-        const Vec v = vec_at(a.vec, (long long)(q.first + c) * a.Hv + h);
-        const int i = 16 * w + 4 * g;
-        gamma = *reinterpret_cast<const f32x4 *>(v.gamma + i);
-        delta = *reinterpret_cast<const f32x4 *>(v.delta + i);
-        beta = *reinterpret_cast<const f32x4 *>(v.beta + i);
-        decay = v.gamma[C - 1];
-    };
-    if (chunks > 0) load_k(0), load_q(0), load_v(0), load_t(0), load_p(0), load_vec(0);
-
-    for (int c = 0; c < chunks; ++c) {
-        // (each array's next values are asked for as soon as its present ones are used up)
-        const int next = min(c + 1, chunks - 1);
-        T *Kc = Ks[c & 1];      // (the other one may still be read)
-        kr.store(Kc);
-        load_k(next);
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) Sp.put4(16 * nt + r16, 16 * (w * DT + dt) + 4 * g, s[dt][nt]);
-        if constexpr (!OUT) {
-            float *S = a.S + ((long long)(q.first + c) * a.Hv + h) * gdelta_state(a) + dv0 * DK;
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<f32x4 *>(S + (16 * nt + r16) * DK + 16 * (w * DT + dt) + 4 * g) = s[dt][nt];
+            since = *reinterpret_cast<const f32x4 *>(vec_at(a.vec, first + (long long)c * a.Hv).gamma + i0);
+        };
+        auto load_p = [&](int c) { pf.load(a.P + (first + (long long)c * a.Hv) * kMatrix, w, lane); };
+        if (x.chunks > 0) {
+            load(0);
+            if constexpr (OUT) load_q(0), load_p(0);
+            store(0);
+            load(min(1, x.chunks - 1));
         }
         __syncthreads();
-
-        f32x4 m[NT], o[NT];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) m[nt] = o[nt] = zero4();
-#pragma unroll
-        for (int t = 0; t < KS; ++t) {
-            const In<T> kf = frag_rows(Kc, KP, 16 * w + r16, 32 * t + 8 * g);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const Of<T, 3> sp = Sp.rows(16 * nt + r16, 32 * t + 8 * g);
-                m[nt] = mma<3>(kf, sp, m[nt]);
-                if constexpr (OUT) o[nt] = mma<2>(qf[t], sp, o[nt]);
-            }
-        }
-        load_q(next);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            f32x4 y;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = beta[e] * ((there[nt] ? to_f32(vv[nt][e]) : 0.f) - gamma[e] * m[nt][e]);
-            *reinterpret_cast<f32x4 *>(Yt + (16 * nt + r16) * YP + 16 * w + 4 * g) = y;
-            if constexpr (OUT) o[nt] *= gamma;
-        }
-        load_v(next);
-        __syncthreads();
-
-        f32x4 u[NT];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            u[nt] = zero4();
-#pragma unroll
-            for (int b = 0; b < 4; ++b)
-                if (b <= w) u[nt] = mma4(tf[b], *reinterpret_cast<const f32x4 *>(Yt + (16 * nt + r16) * YP + 16 * b + 4 * g), u[nt]);
-        }
-        load_t(next);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+        for (int c = 0; c < x.chunks; ++c) {
+            const int next = min(c + 1, x.chunks - 1);
+            __syncthreads();      // parts of K S^T, and S for O
+            f32x4 o = zero4();
             if constexpr (OUT) {
-                Uo.put4(16 * nt + r16, 16 * w + 4 * g, u[nt]);
-            } else {
-                const int wide = (a.dv + 31) / 32 * 32;
-                float *U = a.U + (((long long)(q.first + c) * a.Hv + h) * C + 16 * w + 4 * g) * wide + dv0 + 16 * nt + r16;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) U[e * wide] = u[nt][e];
+                for (int t = 0; t < KS; ++t) o = mma<NPO>(qf[t], Sp.rows(r16, 32 * t + 8 * g), o);
+                o *= since;
+                load_q(next);
             }
-            Ud.put4(16 * nt + r16, 16 * w + 4 * g, u[nt] * delta);
+            __syncthreads();      // Y
+            store(c + 1);
+            load(min(c + 2, x.chunks - 1));
+            __syncthreads();      // U
+            if constexpr (OUT) {
+                auto u = [&](int t) {
+                    f32x8 v;
+                    __builtin_memcpy(&v, __builtin_assume_aligned(Uf + r16 * UP + 32 * t + 8 * g, 16), sizeof(v));
+                    return of<bf16, NPO>(v);
+                };
+                o = mma_parts<NPO>(pf.f[0], u(0), o);
+                if (w >= 2) o = mma_parts<NPO>(pf.f[1], u(1), o);
+                load_p(next);
+                const int len = len_of(c);
+                T *to = O + (long long)(C * c + i0) * a.Hv * a.dv;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (there && i0 + e < len) to[(long long)e * a.Hv * a.dv] = (T)o[e];
+            } else {
+                float *U = a.U + ((first + (long long)c * a.Hv) * C + i0) * wide + x.dv0 + r16;
+                const f32x4 u = *reinterpret_cast<const f32x4 *>(Uf + r16 * UP + i0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) U[e * wide] = u[e];
+            }
         }
-        const float all = decay;
-        load_vec(next);
+        return;
+    }
+
+    // ---- the chain
+    const bool holds = w < Share<DK>::HOLDERS;
+    const int k0 = 32 * w * SLABS + 8 * g;
+    f32x8 s[SLABS];
+#pragma unroll
+    for (int t = 0; t < SLABS; ++t) s[t] = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (a.S0 && there && holds) get_state<FULL>(a.S0 + (x.sh * a.dv + col) * a.dk, k0, a.dk, s);
+    Pairs<3, true> tf;
+    auto load_t = [&](int c) { tf.load(a.T + (first + (long long)c * a.Hv) * kMatrix, w, lane); };
+    if (x.chunks > 0) load_t(0);
+    __syncthreads();
+
+    for (int c = 0; c < x.chunks; ++c) {
+        const int len = len_of(c);
+        const T *Kc = k_tile(c), *Kg = K + (long long)C * c * a.kt;
+        Of<T, 3> sp[SLABS];
+#pragma unroll
+        for (int t = 0; t < SLABS; ++t) sp[t] = of<T, 3>(s[t]);
+        const f32x4 own = products<KTile, T, DK>(Kc, Kg, a.kt, len, a.dk, sp, parts, w, lane);
+        if (holds) {
+            if constexpr (OUT) {
+#pragma unroll
+                for (int t = 0; t < SLABS; ++t) Sp.put8(r16, k0 + 32 * t, sp[t]);
+            } else {
+                put_state<true>(a.S + (first + (long long)c * a.Hv) * gdelta_state(a) + (x.dv0 + r16) * DK, k0, DK, s);
+            }
+        }
         __syncthreads();
 
+        const f32x4 m = joined<DK>(own, parts, w, lane);
+        Yp.put4(r16, i0, bv[w * 64 + lane] - *reinterpret_cast<const f32x4 *>(rate + i0) * m);
+        __syncthreads();
+
+        f32x4 u = mma33(tf.f[0], Yp.rows(r16, 8 * g), zero4());
+        if (w >= 2) u = mma33(tf.f[1], Yp.rows(r16, 32 + 8 * g), u);
+        load_t(min(c + 1, x.chunks - 1));
+        Ud.put4(r16, i0, u * *reinterpret_cast<const f32x4 *>(rate + (2 + (c & 1)) * C + i0));
+        *reinterpret_cast<f32x4 *>(Uf + r16 * UP + i0) = u;
+        const float all = rate[C + (c & 1)];
+        __syncthreads();
+
+        if (holds) {
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
+            for (int t = 0; t < SLABS; ++t) {
+                f32x4 n[2] = {__builtin_shufflevector(s[t], s[t], 0, 1, 2, 3) * all, __builtin_shufflevector(s[t], s[t], 4, 5, 6, 7) * all};
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) s[dt][nt] *= all;
+                for (int b = 0; b < 2; ++b) {
+                    const Of<T, 3> ud = Ud.rows(r16, 32 * b + 8 * g);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            Of<T, 3> ud[NT];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) ud[nt] = Ud.rows(16 * nt + r16, 32 * t + 8 * g);
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                const In<T> kt = frag_cols(Kc, KP, 32 * t + 8 * g, 16 * (w * DT + dt), r16);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) s[dt][nt] = mma<3>(kt, ud[nt], s[dt][nt]);
+                    for (int half = 0; half < 2; ++half)
+                        n[half] = mma<3>(KTile::cols8(Kc, Kg, a.kt, len, a.dk, 32 * b + 8 * g, 32 * (w * SLABS + t), half, r16), ud, n[half]);
+                }
+                s[t] = __builtin_shufflevector(n[0], n[1], 0, 1, 2, 3, 4, 5, 6, 7);
             }
-        }
-        if constexpr (OUT) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-                if (t <= w / 2) {
-                    const Of<T, 2> p = of<T, 2>(pf[t]);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) o[nt] = mma22<T>(p, Uo.rows(16 * nt + r16, 32 * t + 8 * g), o[nt]);
-                }
-            load_p(next);
-            const int len = len_of(c);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = 16 * w + 4 * g + e;
-                    if (there[nt] && i < len) O[(out_row(a, seq, q.tok + C * c + i) * a.Hv + h) * a.dv + col[nt]] = (T)o[nt][e];
-                }
         }
     }
-    if (!OUT || !a.SL) return;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-            if (there[nt]) state4<FULL>(a.SL + ((long long)sh * a.dv + col[nt]) * a.dk, 16 * (w * DT + dt) + 4 * g, a.dk, s[dt][nt]);
+    if (OUT && a.SL && there && holds) put_state<FULL>(a.SL + (x.sh * a.dv + col) * a.dk, k0, a.dk, s);
 }
 
 // Backward, from the last chunk to the first, with R the gradient of the state behind a chunk:
 //   dU = P^T dO + delta K R^T ,  Z = T^T dU ,  dV = beta Z ,  R' = gamma_64 R + (gamma dO)^T Q - (gamma beta Z)^T K .
-// R and Z are kept for the gradients of Q, K and the gates.
-template <typename T, int DK, int NT, bool FULL>
-__global__ __launch_bounds__(256) void scan_bwd_kernel(GDelta a)
+// R and Z are kept for the gradients of Q, K and the gates.  P^T dO and (gamma dO)^T Q are computed beside the chain, a chunk ahead.
+template <typename T, int DK, bool FULL>
+__global__ __launch_bounds__(512) void scan_bwd_kernel(GDelta a)
 {
-    constexpr int KP = pitch<T>(DK), KS = DK / 32, DT = DK / 64, N = 16 * NT, YP = C + 4;
-    typedef Tile<T, 3, N, DK> StateTile;
+    constexpr int OP = pitch<T>(C), SLABS = Share<DK>::SLABS, HOLDERS = Share<DK>::HOLDERS;
     typedef Tile<T, 3, N, C> TokenTile;
-    // (inputs are held once: the barrier behind a chunk is what that costs)
-    __shared__ __attribute__((aligned(16))) T Ks[C * KP], Qs[C * KP];
-    __shared__ __attribute__((aligned(16))) char smem[StateTile::kBytes + 2 * TokenTile::kBytes > N * YP * 4 ? StateTile::kBytes + 2 * TokenTile::kBytes : N * YP * 4];
-    __shared__ __attribute__((aligned(16))) T dOt[N * pitch<T>(C)];
-    const StateTile Rp = {reinterpret_cast<T *>(smem)};
-    const TokenTile Dg = {reinterpret_cast<T *>(smem + StateTile::kBytes)};
-    const TokenTile Zg = {reinterpret_cast<T *>(smem + StateTile::kBytes + TokenTile::kBytes)};
-    float *dUt = reinterpret_cast<float *>(smem);      // in the place of R's parts, once these are used up
+    typedef Tile<bf16, 3, N, C> DUTile;
+    constexpr int kQd = HOLDERS * SLABS * 2 * 1024;
+    constexpr int kWork = 2 * TokenTile::kBytes + DUTile::kBytes + N * OP * (int)sizeof(T) + kQd + (12 + 4 + 4) * 1024 + 4 * C * 4;
+    constexpr int kOne = C * pitch<T>(DK) * (int)sizeof(T);
+    typedef Tokens<T, DK, FULL, 2 * kOne + kWork <= 160 * 1024> KTile;
+    typedef Tokens<T, DK, FULL, 3 * kOne + kWork <= 160 * 1024> QTile;
+    __shared__ __attribute__((aligned(16))) char smem[2 * KTile::kBytes + QTile::kBytes + kWork];
+    char *at = smem + 2 * KTile::kBytes + QTile::kBytes;
+    auto take = [&](int bytes) { char *p = at; at += bytes; return p; };
+    f32x4 *parts = reinterpret_cast<f32x4 *>(take(12 * 1024)), *pd = reinterpret_cast<f32x4 *>(take(4 * 1024));      // pd: P^T dO
+    f32x4 *qd = reinterpret_cast<f32x4 *>(take(kQd)), *zf = reinterpret_cast<f32x4 *>(take(4 * 1024));                // (gamma dO)^T Q; Z
+    float *rate = reinterpret_cast<float *>(take(4 * C * 4));      // delta, gamma_64, gamma beta of even and odd chunks
+    const TokenTile Dg = {reinterpret_cast<T *>(take(TokenTile::kBytes))}, Zg = {reinterpret_cast<T *>(take(TokenTile::kBytes))};
+    const DUTile Du = {reinterpret_cast<bf16 *>(take(DUTile::kBytes))};
+    T *dOt = reinterpret_cast<T *>(at);      // dO, turned
+    auto k_tile = [&](int c) { return reinterpret_cast<T *>(smem + (c & 1) * KTile::kBytes); };
+    T *Qs = reinterpret_cast<T *>(smem + 2 * KTile::kBytes);
 
-    const int wide = (a.dv + 31) / 32 * 32, tiles = wide / N;
-    const int id = (int)xcd_consecutive(blockIdx.x, gridDim.x), tile = id % tiles, sh = id / tiles;
-    const int seq = sh / a.Hv, h = sh - seq * a.Hv, hk = h / (a.Hv / a.Hk), dv0 = tile * N;
-    const Sequence q = sequence_at(a, seq);
-    const int chunks = (q.len + C - 1) / C;
-    const int w = wave_id(), lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4;
+    const int wide = wide_of(a);
+    const Place x = place_of(a, wide / N);
+    const int w = wave_id() & 3, lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4, i0 = 16 * w + 4 * g;
+    const int col = min(x.dv0 + r16, a.dv - 1);
+    const bool there = x.dv0 + r16 < a.dv, holds = w < HOLDERS;
+    const T *K = static_cast<const T *>(a.K) + x.seq * a.kb + x.q.tok * a.kt + x.hk * a.kh;
+    const long long first = (long long)x.q.first * a.Hv + x.h;
+    const int last = x.chunks - 1;
+    auto len_of = [&](int c) { return min(C, x.q.len - C * c); };
 
-    int col[NT];
-    bool there[NT];
+    if (wave_id() >= 4) {      // ---- beside the chain
+        const int thread = threadIdx.x - 256;
+        const T *Q = static_cast<const T *>(a.Q) + x.seq * a.qb + x.q.tok * a.qt + x.hk * a.qh;
+        const T *dO = static_cast<const T *>(a.dO) + x.seq * a.ob + x.q.tok * a.ot + x.h * a.oh + col;
+        T *dV = static_cast<T *>(a.dV) + (out_row(a, x.seq, x.q.tok) * a.Hv + x.h) * a.dv + col;
+        KTile kr;
+        QTile qr;
+        T od[4];
+        f32x4 gamma, delta, beta, now = zero4();      // now: beta of the chunk that the chain is at
+        Pairs<3, false> pf;
+        f32x4 p = zero4(), h[SLABS][2];
+        auto load = [&](int c) {
+            const int len = len_of(c);
+            kr.load(K + (long long)C * c * a.kt, a.kt, len, a.dk, thread);
+            qr.load(Q + (long long)C * c * a.qt, a.qt, len, a.dk, thread);
+            const T *o = dO + (long long)C * c * a.ot;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) col[nt] = min(dv0 + 16 * nt + r16, a.dv - 1), there[nt] = dv0 + 16 * nt + r16 < a.dv;
-    f32x4 s[DT][NT];
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            s[dt][nt] = zero4();
-            if (a.dSL && there[nt]) s[dt][nt] = state4<FULL>(a.dSL + ((long long)sh * a.dv + col[nt]) * a.dk, 16 * (w * DT + dt) + 4 * g, a.dk);
-        }
-
-    const T *K = static_cast<const T *>(a.K) + seq * a.kb + q.tok * a.kt + hk * a.kh;
-    const T *Q = static_cast<const T *>(a.Q) + seq * a.qb + q.tok * a.qt + hk * a.qh;
-    const T *dO = static_cast<const T *>(a.dO) + seq * a.ob + q.tok * a.ot + h * a.oh;
-    T *dV = static_cast<T *>(a.dV);
-
-    Staged<T, DK, FULL> kr, qr;
-    T od[NT][4];
-    f32x4 tf[4], gamma, delta, beta;
-    f32x8 pf[2];
-    float decay = 0.f;
-    auto len_of = [&](int c) { return min(C, q.len - C * c); };
-    auto load_kq = [&](int c) {
-        kr.load(K + (long long)C * c * a.kt, a.kt, len_of(c), a.dk);
-        qr.load(Q + (long long)C * c * a.qt, a.qt, len_of(c), a.dk);
-    };
-    auto load_do = [&](int c) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const T *p = dO + (C * c + min(16 * w + 4 * g + e, len_of(c) - 1)) * a.ot;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) od[nt][e] = p[col[nt]];
-        }
-    };
-    // (columns of T and P: rows of their transposes)
-    auto load_t = [&](int c) {
-        const float *p = a.T + ((long long)(q.first + c) * a.Hv + h) * kMatrix + 4 * g * C + 16 * w + r16;
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-            if (b >= w)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) tf[b][e] = p[(16 * b + e) * C];
-    };
-    auto load_p = [&](int c) {
-        const float *p = a.P + ((long long)(q.first + c) * a.Hv + h) * kMatrix + 8 * g * C + 16 * w + r16;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-            if (b >= w / 2)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) pf[b][e] = p[(32 * b + e) * C];
-    };
-    auto load_vec = [&](int c) {
-        const Vec v = vec_at(a.vec, (long long)(q.first + c) * a.Hv + h);
-        const int i = 16 * w + 4 * g;
-        gamma = *reinterpret_cast<const f32x4 *>(v.gamma + i);
-        delta = *reinterpret_cast<const f32x4 *>(v.delta + i);
-        beta = *reinterpret_cast<const f32x4 *>(v.beta + i);
-        decay = v.gamma[C - 1];
-    };
-    if (chunks > 0) load_kq(chunks - 1), load_do(chunks - 1), load_t(chunks - 1), load_p(chunks - 1), load_vec(chunks - 1);
-
-    for (int c = chunks - 1; c >= 0; --c) {
-        const int next = max(c - 1, 0), len = len_of(c);
-        const long long x = (long long)(q.first + c) * a.Hv + h;
-        kr.store(Ks), qr.store(Qs);
-        load_kq(next);
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                const int k = 16 * (w * DT + dt) + 4 * g;
-                Rp.put4(16 * nt + r16, k, s[dt][nt]);
-                *reinterpret_cast<f32x4 *>(a.R + x * gdelta_state(a) + (dv0 + 16 * nt + r16) * DK + k) = s[dt][nt];
-            }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+            for (int e = 0; e < 4; ++e) od[e] = o[min(i0 + e, len - 1) * a.ot];
+            const Vec v = vec_at(a.vec, first + (long long)c * a.Hv);
+            gamma = *reinterpret_cast<const f32x4 *>(v.gamma + i0);
+            delta = *reinterpret_cast<const f32x4 *>(v.delta + i0);
+            beta = *reinterpret_cast<const f32x4 *>(v.beta + i0);
+        };
+        auto load_p = [&](int c) { pf.load(a.P + (first + (long long)c * a.Hv) * kMatrix, w, lane); };
+        auto store = [&](int c) {
+            kr.store(k_tile(c), thread), qr.store(Qs, thread);
+            const int len = len_of(c);
             f32x4 d;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const bool in = there[nt] && 16 * w + 4 * g + e < len;
-                if (!in) od[nt][e] = (T)0.f;
-                d[e] = gamma[e] * to_f32(od[nt][e]);
+                if (!there || i0 + e >= len) od[e] = (T)0.f;
+                d[e] = gamma[e] * to_f32(od[e]);
             }
-            __builtin_memcpy(dOt + (16 * nt + r16) * pitch<T>(C) + 16 * w + 4 * g, od[nt], sizeof(od[nt]));
-            Dg.put4(16 * nt + r16, 16 * w + 4 * g, d);
-        }
-        load_do(next);
-        __syncthreads();
-
-        f32x4 du[NT];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) du[nt] = zero4();
-#pragma unroll
-        for (int t = 0; t < KS; ++t) {
-            const In<T> kf = frag_rows(Ks, KP, 16 * w + r16, 32 * t + 8 * g);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) du[nt] = mma<3>(kf, Rp.rows(16 * nt + r16, 32 * t + 8 * g), du[nt]);
-        }
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) du[nt] *= delta;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-            if (t >= w / 2) {
-                const Of<T, 3> p = of<T, 3>(pf[t]);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) du[nt] = mma<3>(p, frag_rows(dOt, pitch<T>(C), 16 * nt + r16, 32 * t + 8 * g), du[nt]);
+            __builtin_memcpy(dOt + r16 * OP + i0, od, sizeof(od));
+            Dg.put4(r16, i0, d);
+            if (r16 == 0) {
+                *reinterpret_cast<f32x4 *>(rate + i0) = delta;
+                *reinterpret_cast<f32x4 *>(rate + (2 + (c & 1)) * C + i0) = -gamma * beta;
+                if (w == 3 && g == 3) rate[C + (c & 1)] = gamma[3];
             }
-        load_p(next);
-        __syncthreads();
+        };
+        auto multiply = [&](int c) {
+            const T *Qg = Q + (long long)C * c * a.qt;
+            const int len = len_of(c);
+            p = zero4();
+            if (w < 2) p = mma_input(pf.f[0], frag_rows(dOt, OP, r16, 8 * g), p);
+            p = mma_input(pf.f[1], frag_rows(dOt, OP, r16, 32 + 8 * g), p);
+            if (!holds) return;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<f32x4 *>(dUt + (16 * nt + r16) * YP + 16 * w + 4 * g) = du[nt];
-        __syncthreads();
-
-        f32x4 z[NT];
+            for (int t = 0; t < SLABS; ++t) {
+                h[t][0] = h[t][1] = zero4();
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            z[nt] = zero4();
+                for (int b = 0; b < 2; ++b) {
+                    const Of<T, 3> d = Dg.rows(r16, 32 * b + 8 * g);
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
-                if (b >= w) z[nt] = mma4(tf[b], *reinterpret_cast<const f32x4 *>(dUt + (16 * nt + r16) * YP + 16 * b + 4 * g), z[nt]);
-        }
-        load_t(next);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            float *Z = a.Z + (x * C + 16 * w + 4 * g) * wide + dv0 + 16 * nt + r16;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int i = 16 * w + 4 * g + e;
-                Z[e * wide] = z[nt][e];
-                const float d = beta[e] * z[nt][e];
-                if (there[nt] && i < len) dV[(out_row(a, seq, q.tok + C * c + i) * a.Hv + h) * a.dv + col[nt]] = (T)d;
-                z[nt][e] = -gamma[e] * d;
-            }
-            Zg.put4(16 * nt + r16, 16 * w + 4 * g, z[nt]);
-        }
-        const float all = decay;
-        load_vec(next);
-        __syncthreads();
-
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) s[dt][nt] *= all;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            Of<T, 3> dg[NT], zg[NT];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) dg[nt] = Dg.rows(16 * nt + r16, 32 * t + 8 * g), zg[nt] = Zg.rows(16 * nt + r16, 32 * t + 8 * g);
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
-                const In<T> qt = frag_cols(Qs, KP, 32 * t + 8 * g, 16 * (w * DT + dt), r16);
-                const In<T> kt = frag_cols(Ks, KP, 32 * t + 8 * g, 16 * (w * DT + dt), r16);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    s[dt][nt] = mma<3>(qt, dg[nt], s[dt][nt]);
-                    s[dt][nt] = mma<3>(kt, zg[nt], s[dt][nt]);
+                    for (int half = 0; half < 2; ++half)
+                        h[t][half] = mma<3>(QTile::cols8(Qs, Qg, a.qt, len, a.dk, 32 * b + 8 * g, 32 * (w * SLABS + t), half, r16), d, h[t][half]);
                 }
             }
+        };
+        if (last >= 0) {
+            load(last), load_p(last);
+            store(last);
+            now = beta;
+            load(max(last - 1, 0));
         }
         __syncthreads();
+        if (last >= 0) {
+            multiply(last);
+            load_p(max(last - 1, 0));
+            pd[w * 64 + lane] = p;
+        }
+        __syncthreads();
+        for (int c = last; c >= 0; --c) {
+            const int next = max(c - 1, 0), len = len_of(c);      // (before the first chunk the same again, which nobody takes)
+            __syncthreads();      // parts of K R^T
+            if (holds) {
+#pragma unroll
+                for (int t = 0; t < SLABS; ++t)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) qd[((w * SLABS + t) * 2 + half) * 64 + lane] = h[t][half];
+            }
+            __syncthreads();      // dU
+            const f32x4 then = beta;
+            if (c > 0) store(next);
+            load(max(c - 2, 0));
+            __syncthreads();      // Z
+            const f32x4 z = zf[w * 64 + lane];
+            float *Z = a.Z + ((first + (long long)c * a.Hv) * C + i0) * wide + x.dv0 + r16;
+            T *to = dV + (long long)(C * c + i0) * a.Hv * a.dv;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                Z[e * wide] = z[e];
+                if (there && i0 + e < len) to[(long long)e * a.Hv * a.dv] = (T)(now[e] * z[e]);
+            }
+            now = then;
+            multiply(next);
+            load_p(max(c - 2, 0));
+            pd[w * 64 + lane] = p;
+        }
+        return;
     }
-    if (!a.dS0) return;
+
+    // ---- the chain
+    const int k0 = 32 * w * SLABS + 8 * g;
+    f32x8 s[SLABS];
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
+    for (int t = 0; t < SLABS; ++t) s[t] = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (a.dSL && there && holds) get_state<FULL>(a.dSL + (x.sh * a.dv + col) * a.dk, k0, a.dk, s);
+    Pairs<3, false> tf;
+    auto load_t = [&](int c) { tf.load(a.Tt + (first + (long long)c * a.Hv) * kMatrix, w, lane); };
+    if (last >= 0) load_t(last);
+    __syncthreads();
+    __syncthreads();
+
+    for (int c = last; c >= 0; --c) {
+        const int len = len_of(c);
+        const T *Kc = k_tile(c), *Kg = K + (long long)C * c * a.kt;
+        Of<T, 3> sp[SLABS];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-            if (there[nt]) state4<FULL>(a.dS0 + ((long long)sh * a.dv + col[nt]) * a.dk, 16 * (w * DT + dt) + 4 * g, a.dk, s[dt][nt]);
+        for (int t = 0; t < SLABS; ++t) sp[t] = of<T, 3>(s[t]);
+        const f32x4 own = products<KTile, T, DK>(Kc, Kg, a.kt, len, a.dk, sp, parts, w, lane);
+        if (holds) put_state<true>(a.R + (first + (long long)c * a.Hv) * gdelta_state(a) + (x.dv0 + r16) * DK, k0, DK, s);
+        __syncthreads();
+
+        Du.put4(r16, i0, joined<DK>(own, parts, w, lane) * *reinterpret_cast<const f32x4 *>(rate + i0) + pd[w * 64 + lane]);
+        __syncthreads();
+
+        f32x4 z = mma33(tf.f[1], Du.rows(r16, 32 + 8 * g), zero4());
+        if (w < 2) z = mma33(tf.f[0], Du.rows(r16, 8 * g), z);
+        load_t(max(c - 1, 0));
+        Zg.put4(r16, i0, z * *reinterpret_cast<const f32x4 *>(rate + (2 + (c & 1)) * C + i0));
+        zf[w * 64 + lane] = z;
+        const float all = rate[C + (c & 1)];
+        __syncthreads();
+
+        if (holds) {
+#pragma unroll
+            for (int t = 0; t < SLABS; ++t) {
+                const f32x4 *q = qd + (w * SLABS + t) * 2 * 64 + lane;
+                f32x4 n[2] = {__builtin_shufflevector(s[t], s[t], 0, 1, 2, 3) * all + q[0], __builtin_shufflevector(s[t], s[t], 4, 5, 6, 7) * all + q[64]};
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const Of<T, 3> zg = Zg.rows(r16, 32 * b + 8 * g);
+#pragma unroll
+                    for (int half = 0; half < 2; ++half)
+                        n[half] = mma<3>(KTile::cols8(Kc, Kg, a.kt, len, a.dk, 32 * b + 8 * g, 32 * (w * SLABS + t), half, r16), zg, n[half]);
+                }
+                s[t] = __builtin_shufflevector(n[0], n[1], 0, 1, 2, 3, 4, 5, 6, 7);
+            }
+        }
+    }
+    if (a.dS0 && there && holds) put_state<FULL>(a.dS0 + (x.sh * a.dv + col) * a.dk, k0, a.dk, s);
 }
 
 enum { kForward, kKeep, kBackward };
 
-template <typename T, int DK, int NT> hipError_t scan(const GDelta &a, bool full, int what, hipStream_t stream)
+template <typename T, int DK> hipError_t scan(const GDelta &a, bool full, int what, hipStream_t stream)
 {
-    const int tiles = what == kForward ? (a.dv + 16 * NT - 1) / (16 * NT) : (a.dv + 31) / 32 * (2 / NT);
+    const int tiles = what == kForward ? (a.dv + N - 1) / N : (a.dv + 31) / 32 * 2;
     const double groups = (double)a.N * a.Hv * tiles;
-    if (!launch_holds(groups, 256)) return hipErrorInvalidConfiguration;
+    if (!launch_holds(groups, 512)) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)groups);
     if (what == kForward)
-        full ? scan_kernel<T, DK, NT, true, true><<<grid, 256, 0, stream>>>(a) : scan_kernel<T, DK, NT, false, true><<<grid, 256, 0, stream>>>(a);
+        full ? scan_kernel<T, DK, true, true><<<grid, 512, 0, stream>>>(a) : scan_kernel<T, DK, false, true><<<grid, 512, 0, stream>>>(a);
     else if (what == kKeep)
-        full ? scan_kernel<T, DK, NT, true, false><<<grid, 256, 0, stream>>>(a) : scan_kernel<T, DK, NT, false, false><<<grid, 256, 0, stream>>>(a);
+        full ? scan_kernel<T, DK, true, false><<<grid, 512, 0, stream>>>(a) : scan_kernel<T, DK, false, false><<<grid, 512, 0, stream>>>(a);
     else
-        full ? scan_bwd_kernel<T, DK, NT, true><<<grid, 256, 0, stream>>>(a) : scan_bwd_kernel<T, DK, NT, false><<<grid, 256, 0, stream>>>(a);
+        full ? scan_bwd_kernel<T, DK, true><<<grid, 512, 0, stream>>>(a) : scan_bwd_kernel<T, DK, false><<<grid, 512, 0, stream>>>(a);
     return hipGetLastError();
 }
 template <typename T> hipError_t scan(const GDelta &a, int what, hipStream_t stream)
 {
     const bool full = gdelta_full(a, sizeof(T));
-    return a.dk <= 64 ? scan<T, 64, 1>(a, full, what, stream) : a.dk <= 128 ? scan<T, 128, 1>(a, full, what, stream) : scan<T, 256, 1>(a, full, what, stream);
+    return a.dk <= 64 ? scan<T, 64>(a, full, what, stream) : a.dk <= 128 ? scan<T, 128>(a, full, what, stream) : scan<T, 256>(a, full, what, stream);
 }
 
 }  // namespace

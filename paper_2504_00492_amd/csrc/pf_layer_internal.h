@@ -81,7 +81,8 @@ struct GDelta {
     long long rows;          // rows of the outputs from one sequence to the next (packed: none)
     int per, chunks;         // chunks of a sequence (not of packed ones) and all together, or as many as there can be
     int *plan;               // the workspace's parts, set by gdelta_workspace
-    float *T, *P, *vec, *S, *U, *Z, *R;
+    __bf16 *T, *P, *Tt;      // Tt: backward
+    float *vec, *S, *U, *Z, *R;
 };
 // d_k is padded with zeros to a width that the kernels have
 __host__ __device__ inline int gdelta_width(int dk) { return dk <= 64 ? 64 : dk <= 128 ? 128 : 256; }
