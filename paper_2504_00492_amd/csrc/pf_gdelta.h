@@ -63,6 +63,21 @@ template <int USE, int NP, typename T> __device__ __forceinline__ f32x4 mma(cons
         return c;
     }
 }
+// N results side by side, c += a b for one b: a product that adds to the result of the one before it waits for that
+template <typename T, int N> __device__ __forceinline__ void mma_each(const In<T> (&a)[N], const Of<T, 3> &b, f32x4 (&c)[N])
+{
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int i = 0; i < N; ++i) c[i] = mfma4(a[i].v[e], b.v[e], c[i]);
+    } else {
+#pragma unroll
+        for (int p = 2; p >= 0; --p)
+#pragma unroll
+            for (int i = 0; i < N; ++i) c[i] = mfma16(a[i].v, b.p[p], c[i]);
+    }
+}
 // two computed numbers of two parts each: the product of the small parts is left out (2^-18)
 template <typename T> __device__ __forceinline__ f32x4 mma22(const Of<T, 2> &a, const Of<T, 2> &b, f32x4 c)
 {
@@ -75,6 +90,7 @@ template <typename T> __device__ __forceinline__ f32x4 mma22(const Of<T, 2> &a, 
     }
 }
 
+__device__ __forceinline__ f32x8 stack(f32x4 a, f32x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 // three parts each: what is left out is 2^-24 of the whole
 __device__ __forceinline__ f32x4 mma33(const Of<bf16, 3> &a, const Of<bf16, 3> &b, f32x4 c)
 {
@@ -232,15 +248,18 @@ struct Plan {
 };
 __host__ __device__ inline Plan plan_of(int *p, int N) { return {p, p + N, p + 2 * N, p + 3 * N}; }
 
+// (what is the same for a whole wavefront, in scalar registers: addresses that come from it cost the vector unit nothing)
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 __device__ __forceinline__ bool chunk_at(const GDelta &a, int id, Chunk &x)
 {
     if (a.offsets) {
         const Plan p = plan_of(a.plan, a.N);
-        x.seq = p.of[id];
+        x.seq = uniform(p.of[id]);
         if (x.seq < 0) return false;
-        x.c = id - p.first[x.seq];
-        x.tok = p.start[x.seq] + C * x.c;
-        x.len = min(C, p.len[x.seq] - C * x.c);
+        x.c = id - uniform(p.first[x.seq]);
+        x.tok = uniform(p.start[x.seq]) + C * x.c;
+        x.len = min(C, uniform(p.len[x.seq]) - C * x.c);
     } else {
         x.seq = id / a.per;
         x.c = id - x.seq * a.per;
@@ -257,7 +276,7 @@ __device__ __forceinline__ Sequence sequence_at(const GDelta &a, int seq)
     if (a.offsets) {
         if (a.chunks == 0) return {0, 0, 0};
         const Plan p = plan_of(a.plan, a.N);
-        return {p.start[seq], p.len[seq], p.first[seq]};
+        return {uniform(p.start[seq]), uniform(p.len[seq]), uniform(p.first[seq])};
     }
     return {0, a.L, seq * a.per};
 }

@@ -60,7 +60,7 @@ template <typename T, int DK, bool FULL, bool LDS> struct Tokens {
             }
         }
     }
-    static __device__ __forceinline__ In<T> rows(const T *tile, const T *p, long long step, int len, int dk, int row, int k)
+    static __device__ __forceinline__ In<T> row_frag(const T *tile, const T *p, long long step, int len, int dk, int row, int k)
     {
         if constexpr (LDS) return frag_rows(tile, kLd, row, k);
         else return fetch<T, FULL>(p + min(row, len - 1) * step + k, dk - k);
@@ -103,7 +103,7 @@ __device__ __forceinline__ Place place_of(const GDelta &a, int tiles)
 {
     // tiles of one head side by side, on one XCD: they read the same K, Q, T and P
     Place x;
-    const int id = (int)xcd_consecutive(blockIdx.x, gridDim.x), sh = id / tiles;
+    const int id = uniform((int)xcd_consecutive(blockIdx.x, gridDim.x)), sh = id / tiles;
     x.sh = sh;
     x.seq = sh / a.Hv, x.h = sh - x.seq * a.Hv, x.hk = x.h / (a.Hv / a.Hk), x.dv0 = (id - sh * tiles) * N;
     x.q = sequence_at(a, x.seq);
@@ -134,22 +134,37 @@ template <bool FULL, int SLABS> __device__ __forceinline__ void put_state(float 
     }
 }
 
-// Tokens times the transposed state: each holder multiplies what it has of d_k for all 64 tokens, with the tiles of 16 tokens counted
-// from its own (w ^ i), so that registers are named at compile time; the others' parts go through LDS (1 KB as the lanes hold it).
-template <typename K, typename T, int DK>
-__device__ __forceinline__ f32x4 products(const T *Kc, const T *Kg, long long step, int len, int dk, const Of<T, 3> (&sp)[Share<DK>::SLABS],
-                                          f32x4 *parts, int w, int lane)
-{
-    const int r16 = lane & 15, g = lane >> 4;
-    f32x4 m[4];
+// Fragments of a chunk's tokens for a wavefront of the chain: for each of its 32 of d_k the rows of the four tiles of 16 tokens, counted from its
+// own (w ^ i), so that registers are named at compile time; and the columns, of the first and the last 32 tokens.
+template <typename T, int SLABS> struct Fragments {
+    In<T> f[SLABS][4];
+    template <typename K> __device__ __forceinline__ void rows(const T *tile, const T *p, long long step, int len, int dk, int w, int lane)
+    {
+        const int r16 = lane & 15, g = lane >> 4;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) m[i] = zero4();
+        for (int t = 0; t < SLABS; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[t][i] = K::row_frag(tile, p, step, len, dk, 16 * (w ^ i) + r16, 32 * (w * SLABS + t) + 8 * g);
+    }
+    template <typename K> __device__ __forceinline__ void cols(const T *tile, const T *p, long long step, int len, int dk, int w, int lane)
+    {
+        const int r16 = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int t = 0; t < SLABS; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[t][i] = K::cols8(tile, p, step, len, dk, 32 * (i >> 1) + 8 * g, 32 * (w * SLABS + t), i & 1, r16);
+    }
+};
+
+// Tokens times the transposed state: each holder multiplies what it has of d_k for all 64 tokens; the others' parts go through LDS (1 KB
+// as the lanes hold it).
+template <typename T, int DK>
+__device__ __forceinline__ f32x4 products(const Fragments<T, Share<DK>::SLABS> &k, const Of<T, 3> (&sp)[Share<DK>::SLABS], f32x4 *parts, int w, int lane)
+{
+    f32x4 m[4] = {zero4(), zero4(), zero4(), zero4()};
     if (w < Share<DK>::HOLDERS) {
 #pragma unroll
-        for (int t = 0; t < Share<DK>::SLABS; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                m[i] = mma<3>(K::rows(Kc, Kg, step, len, dk, 16 * (w ^ i) + r16, 32 * (w * Share<DK>::SLABS + t) + 8 * g), sp[t], m[i]);
+        for (int t = 0; t < Share<DK>::SLABS; ++t) mma_each(k.f[t], sp[t], m);
 #pragma unroll
         for (int i = 1; i < 4; ++i) parts[((w ^ i) * 3 + i - 1) * 64 + lane] = m[i];
     }
@@ -160,6 +175,32 @@ template <int DK> __device__ __forceinline__ f32x4 joined(f32x4 own, const f32x4
     const f32x4 *p = parts + w * 3 * 64 + lane;
     if constexpr (Share<DK>::HOLDERS == 4) return (own + p[0]) + (p[64] + p[128]);
     else return w < 2 ? own + p[0] : p[64] + p[128];
+}
+// s = all s + (h, if any) + tokens^T x, x[2] of the first and the last 32 tokens
+template <typename T, int SLABS>
+__device__ __forceinline__ void update(f32x8 (&s)[SLABS], float all, const f32x4 *h, const Fragments<T, SLABS> &k, const Of<T, 3> (&x)[2])
+{
+#pragma unroll
+    for (int t = 0; t < SLABS; ++t) {
+        f32x4 n[2] = {__builtin_shufflevector(s[t], s[t], 0, 1, 2, 3) * all, __builtin_shufflevector(s[t], s[t], 4, 5, 6, 7) * all}, l[2] = {zero4(), zero4()};
+        if (h) l[0] = h[t * 128], l[1] = h[t * 128 + 64];
+        const In<T> a[2] = {k.f[t][0], k.f[t][1]}, b[2] = {k.f[t][2], k.f[t][3]};
+        mma_each(a, x[0], n);
+        mma_each(b, x[1], l);
+        s[t] = stack(n[0] + l[0], n[1] + l[1]);
+    }
+}
+// Four neighbouring values of a row of the outputs, of which `left` are there.  WHOLE: rows are whole and lie at multiples of their size.
+template <typename T> __device__ __forceinline__ void put_row(T *to, f32x4 v, int left, bool whole)
+{
+    typedef T t4 __attribute__((ext_vector_type(4)));
+    if (whole) {
+        *reinterpret_cast<t4 *>(to) = __builtin_convertvector(v, t4);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) to[e] = (T)v[e];
+    }
 }
 
 // Forward.  OUT: O is wanted; else the states before every chunk and U are kept for the backward.
@@ -195,12 +236,16 @@ __global__ __launch_bounds__(512) void scan_kernel(GDelta a)
         const int thread = threadIdx.x - 256, wide = wide_of(a);
         const T *Q = static_cast<const T *>(a.Q) + x.seq * a.qb + x.q.tok * a.qt + x.hk * a.qh;
         const T *V = static_cast<const T *>(a.V) + x.seq * a.vb + x.q.tok * a.vt + x.h * a.vh + col;
-        T *O = static_cast<T *>(a.O) + (out_row(a, x.seq, x.q.tok) * a.Hv + x.h) * a.dv + col;
+        // O of token 16 w + r16, rows 4 g .. of the 16
+        const int t0 = 16 * w + r16, left = a.dv - x.dv0 - 4 * g;      // (or U's)
+        const bool whole = a.dv % 4 == 0;
+        T *O = static_cast<T *>(a.O) + ((out_row(a, x.seq, x.q.tok) + t0) * a.Hv + x.h) * a.dv + x.dv0 + 4 * g;
         KTile kr;
         In<T> qf[KS];
         T vv[4];
         Pairs<NPO, true> pf;
-        f32x4 gamma, beta, delta, since;
+        f32x4 gamma, beta, delta;
+        float since = 0.f;
         auto load = [&](int c) {      // what the chain takes
             kr.load(K + (long long)C * c * a.kt, a.kt, len_of(c), a.dk, thread);
             const T *p = V + (long long)C * c * a.vt;
@@ -228,7 +273,7 @@ __global__ __launch_bounds__(512) void scan_kernel(GDelta a)
             const T *p = Q + (C * c + min(16 * w + r16, len_of(c) - 1)) * a.qt;
 #pragma unroll
             for (int t = 0; t < KS; ++t) qf[t] = fetch<T, FULL>(p + 32 * t + 8 * g, a.dk - 32 * t - 8 * g);
-            since = *reinterpret_cast<const f32x4 *>(vec_at(a.vec, first + (long long)c * a.Hv).gamma + i0);
+            since = vec_at(a.vec, first + (long long)c * a.Hv).gamma[t0];
         };
         auto load_p = [&](int c) { pf.load(a.P + (first + (long long)c * a.Hv) * kMatrix, w, lane); };
         if (x.chunks > 0) {
@@ -241,11 +286,11 @@ __global__ __launch_bounds__(512) void scan_kernel(GDelta a)
         for (int c = 0; c < x.chunks; ++c) {
             const int next = min(c + 1, x.chunks - 1);
             __syncthreads();      // parts of K S^T, and S for O
-            f32x4 o = zero4();
+            f32x4 o[2] = {zero4(), zero4()};
             if constexpr (OUT) {
 #pragma unroll
-                for (int t = 0; t < KS; ++t) o = mma<NPO>(qf[t], Sp.rows(r16, 32 * t + 8 * g), o);
-                o *= since;
+                for (int t = 0; t < KS; ++t) o[t & 1] = mma<NPO>(Sp.rows(r16, 32 * t + 8 * g), qf[t], o[t & 1]);
+                o[0] = (o[0] + o[1]) * since;
                 load_q(next);
             }
             __syncthreads();      // Y
@@ -258,19 +303,13 @@ __global__ __launch_bounds__(512) void scan_kernel(GDelta a)
                     __builtin_memcpy(&v, __builtin_assume_aligned(Uf + r16 * UP + 32 * t + 8 * g, 16), sizeof(v));
                     return of<bf16, NPO>(v);
                 };
-                o = mma_parts<NPO>(pf.f[0], u(0), o);
-                if (w >= 2) o = mma_parts<NPO>(pf.f[1], u(1), o);
+                o[1] = mma_parts<NPO>(u(0), pf.f[0], zero4());
+                if (w >= 2) o[0] = mma_parts<NPO>(u(1), pf.f[1], o[0]);
                 load_p(next);
-                const int len = len_of(c);
-                T *to = O + (long long)(C * c + i0) * a.Hv * a.dv;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (there && i0 + e < len) to[(long long)e * a.Hv * a.dv] = (T)o[e];
+                if (t0 < len_of(c) && left > 0) put_row(O + (long long)C * c * a.Hv * a.dv, o[0] + o[1], left, whole);
             } else {
-                float *U = a.U + ((first + (long long)c * a.Hv) * C + i0) * wide + x.dv0 + r16;
-                const f32x4 u = *reinterpret_cast<const f32x4 *>(Uf + r16 * UP + i0);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) U[e * wide] = u[e];
+                const float *u = Uf + 4 * g * UP + t0;
+                *reinterpret_cast<f32x4 *>(a.U + ((first + (long long)c * a.Hv) * C + t0) * wide + x.dv0 + 4 * g) = f32x4{u[0], u[UP], u[2 * UP], u[3 * UP]};
             }
         }
         return;
@@ -287,14 +326,18 @@ __global__ __launch_bounds__(512) void scan_kernel(GDelta a)
     auto load_t = [&](int c) { tf.load(a.T + (first + (long long)c * a.Hv) * kMatrix, w, lane); };
     if (x.chunks > 0) load_t(0);
     __syncthreads();
+    Fragments<T, SLABS> kf, kc;
+    auto rows = [&](int c) { kf.template rows<KTile>(k_tile(c), K + (long long)C * c * a.kt, a.kt, len_of(c), a.dk, w, lane); };
+    auto cols = [&](int c) { kc.template cols<KTile>(k_tile(c), K + (long long)C * c * a.kt, a.kt, len_of(c), a.dk, w, lane); };
+    constexpr bool AHEAD = KTile::kBytes > 0;      // (out of memory they are taken where they are used: there are no registers for more)
+    if (AHEAD && x.chunks > 0 && holds) rows(0);
 
     for (int c = 0; c < x.chunks; ++c) {
-        const int len = len_of(c);
-        const T *Kc = k_tile(c), *Kg = K + (long long)C * c * a.kt;
+        if (!AHEAD && holds) rows(c);
         Of<T, 3> sp[SLABS];
 #pragma unroll
         for (int t = 0; t < SLABS; ++t) sp[t] = of<T, 3>(s[t]);
-        const f32x4 own = products<KTile, T, DK>(Kc, Kg, a.kt, len, a.dk, sp, parts, w, lane);
+        const f32x4 own = products<T, DK>(kf, sp, parts, w, lane);
         if (holds) {
             if constexpr (OUT) {
 #pragma unroll
@@ -310,26 +353,19 @@ __global__ __launch_bounds__(512) void scan_kernel(GDelta a)
         __syncthreads();
 
         f32x4 u = mma33(tf.f[0], Yp.rows(r16, 8 * g), zero4());
-        if (w >= 2) u = mma33(tf.f[1], Yp.rows(r16, 32 + 8 * g), u);
+        if (w >= 2) u += mma33(tf.f[1], Yp.rows(r16, 32 + 8 * g), zero4());
         load_t(min(c + 1, x.chunks - 1));
         Ud.put4(r16, i0, u * *reinterpret_cast<const f32x4 *>(rate + (2 + (c & 1)) * C + i0));
         *reinterpret_cast<f32x4 *>(Uf + r16 * UP + i0) = u;
         const float all = rate[C + (c & 1)];
+        if (AHEAD && holds) cols(c);
         __syncthreads();
 
         if (holds) {
-#pragma unroll
-            for (int t = 0; t < SLABS; ++t) {
-                f32x4 n[2] = {__builtin_shufflevector(s[t], s[t], 0, 1, 2, 3) * all, __builtin_shufflevector(s[t], s[t], 4, 5, 6, 7) * all};
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const Of<T, 3> ud = Ud.rows(r16, 32 * b + 8 * g);
-#pragma unroll
-                    for (int half = 0; half < 2; ++half)
-                        n[half] = mma<3>(KTile::cols8(Kc, Kg, a.kt, len, a.dk, 32 * b + 8 * g, 32 * (w * SLABS + t), half, r16), ud, n[half]);
-                }
-                s[t] = __builtin_shufflevector(n[0], n[1], 0, 1, 2, 3, 4, 5, 6, 7);
-            }
+            const Of<T, 3> ud[2] = {Ud.rows(r16, 8 * g), Ud.rows(r16, 32 + 8 * g)};
+            if (!AHEAD) cols(c);
+            else if (c + 1 < x.chunks) rows(c + 1);
+            update<T, SLABS>(s, all, nullptr, kc, ud);
         }
     }
     if (OUT && a.SL && there && holds) put_state<FULL>(a.SL + (x.sh * a.dv + col) * a.dk, k0, a.dk, s);
@@ -338,14 +374,14 @@ __global__ __launch_bounds__(512) void scan_kernel(GDelta a)
 // Backward, from the last chunk to the first, with R the gradient of the state behind a chunk:
 //   dU = P^T dO + delta K R^T ,  Z = T^T dU ,  dV = beta Z ,  R' = gamma_64 R + (gamma dO)^T Q - (gamma beta Z)^T K .
 // R and Z are kept for the gradients of Q, K and the gates.  P^T dO and (gamma dO)^T Q are computed beside the chain, a chunk ahead.
-template <typename T, int DK, bool FULL>
-__global__ __launch_bounds__(512) void scan_bwd_kernel(GDelta a)
+template <typename T, int DK, bool FULL, int GROUPS>
+__global__ __launch_bounds__(256 * GROUPS) void scan_bwd_kernel(GDelta a)
 {
-    constexpr int OP = pitch<T>(C), SLABS = Share<DK>::SLABS, HOLDERS = Share<DK>::HOLDERS;
+    constexpr int OP = pitch<T>(C), XP = C + 4, SLABS = Share<DK>::SLABS, HOLDERS = Share<DK>::HOLDERS;
     typedef Tile<T, 3, N, C> TokenTile;
     typedef Tile<bf16, 3, N, C> DUTile;
     constexpr int kQd = HOLDERS * SLABS * 2 * 1024;
-    constexpr int kWork = 2 * TokenTile::kBytes + DUTile::kBytes + N * OP * (int)sizeof(T) + kQd + (12 + 4 + 4) * 1024 + 4 * C * 4;
+    constexpr int kWork = 2 * TokenTile::kBytes + DUTile::kBytes + N * OP * (int)sizeof(T) + kQd + (12 + 4) * 1024 + N * XP * 4 + 4 * C * 4;
     constexpr int kOne = C * pitch<T>(DK) * (int)sizeof(T);
     typedef Tokens<T, DK, FULL, 2 * kOne + kWork <= 160 * 1024> KTile;
     typedef Tokens<T, DK, FULL, 3 * kOne + kWork <= 160 * 1024> QTile;
@@ -353,7 +389,8 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(GDelta a)
     char *at = smem + 2 * KTile::kBytes + QTile::kBytes;
     auto take = [&](int bytes) { char *p = at; at += bytes; return p; };
     f32x4 *parts = reinterpret_cast<f32x4 *>(take(12 * 1024)), *pd = reinterpret_cast<f32x4 *>(take(4 * 1024));      // pd: P^T dO
-    f32x4 *qd = reinterpret_cast<f32x4 *>(take(kQd)), *zf = reinterpret_cast<f32x4 *>(take(4 * 1024));                // (gamma dO)^T Q; Z
+    f32x4 *qd = reinterpret_cast<f32x4 *>(take(kQd));                // (gamma dO)^T Q
+    float *zf = reinterpret_cast<float *>(take(N * XP * 4));           // Z, turned
     float *rate = reinterpret_cast<float *>(take(4 * C * 4));      // delta, gamma_64, gamma beta of even and odd chunks
     const TokenTile Dg = {reinterpret_cast<T *>(take(TokenTile::kBytes))}, Zg = {reinterpret_cast<T *>(take(TokenTile::kBytes))};
     const DUTile Du = {reinterpret_cast<bf16 *>(take(DUTile::kBytes))};
@@ -372,14 +409,26 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(GDelta a)
     auto len_of = [&](int c) { return min(C, x.q.len - C * c); };
 
     if (wave_id() >= 4) {      // ---- beside the chain
-        const int thread = threadIdx.x - 256;
+        const int thread = threadIdx.x & 255;
+        const bool carry = GROUPS == 2 || wave_id() < 8, read = GROUPS == 2 || wave_id() >= 8;
         const T *Q = static_cast<const T *>(a.Q) + x.seq * a.qb + x.q.tok * a.qt + x.hk * a.qh;
         const T *dO = static_cast<const T *>(a.dO) + x.seq * a.ob + x.q.tok * a.ot + x.h * a.oh + col;
-        T *dV = static_cast<T *>(a.dV) + (out_row(a, x.seq, x.q.tok) * a.Hv + x.h) * a.dv + col;
+        const int t0 = 16 * w + r16, left = a.dv - x.dv0 - 4 * g;      // Z and dV of this token, rows 4 g .. of the 16
+        const bool whole = a.dv % 4 == 0;
+        T *dV = static_cast<T *>(a.dV) + ((out_row(a, x.seq, x.q.tok) + t0) * a.Hv + x.h) * a.dv + x.dv0 + 4 * g;
         KTile kr;
         QTile qr;
         T od[4];
-        f32x4 gamma, delta, beta, now = zero4();      // now: beta of the chunk that the chain is at
+        f32x4 gamma, delta, beta;
+        float rate_of = 0.f, next_rate = 0.f, now = 0.f;      // beta of this lane's token: as loaded, and of the next two chunks to be stored
+        f32x4 z = zero4();
+        // Z and dV are stored at once, or by a group of their own a chunk later: memory answers in order, so what waits for its loads of P
+        // waits for the stores before them, which are a chunk old then (both at d = 128: 491 -> 373 us; of two groups, d = 64: 64 and 82).
+        constexpr bool LATER = GROUPS == 3;
+        auto put = [&](int c) {
+            *reinterpret_cast<f32x4 *>(a.Z + ((first + (long long)c * a.Hv) * C + t0) * wide + x.dv0 + 4 * g) = z;
+            if (t0 < len_of(c) && left > 0) put_row(dV + (long long)C * c * a.Hv * a.dv, now * z, left, whole);
+        };
         Pairs<3, false> pf;
         f32x4 p = zero4(), h[SLABS][2];
         auto load = [&](int c) {
@@ -394,7 +443,10 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(GDelta a)
             delta = *reinterpret_cast<const f32x4 *>(v.delta + i0);
             beta = *reinterpret_cast<const f32x4 *>(v.beta + i0);
         };
-        auto load_p = [&](int c) { pf.load(a.P + (first + (long long)c * a.Hv) * kMatrix, w, lane); };
+        auto load_p = [&](int c) {
+            pf.load(a.P + (first + (long long)c * a.Hv) * kMatrix, w, lane);
+            rate_of = vec_at(a.vec, first + (long long)c * a.Hv).beta[t0];
+        };
         auto store = [&](int c) {
             kr.store(k_tile(c), thread), qr.store(Qs, thread);
             const int len = len_of(c);
@@ -431,46 +483,49 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(GDelta a)
                 }
             }
         };
-        if (last >= 0) {
-            load(last), load_p(last);
+        if (last >= 0 && read) load_p(last);
+        if (last >= 0 && carry) {
+            load(last);
             store(last);
-            now = beta;
             load(max(last - 1, 0));
         }
         __syncthreads();
-        if (last >= 0) {
+        if (last >= 0 && read) {
             multiply(last);
+            now = next_rate = rate_of;
             load_p(max(last - 1, 0));
             pd[w * 64 + lane] = p;
         }
         __syncthreads();
         for (int c = last; c >= 0; --c) {
-            const int next = max(c - 1, 0), len = len_of(c);      // (before the first chunk the same again, which nobody takes)
+            const int next = max(c - 1, 0);      // (before the first chunk the same again, which nobody takes)
             __syncthreads();      // parts of K R^T
-            if (holds) {
+            if (holds && read) {
 #pragma unroll
                 for (int t = 0; t < SLABS; ++t)
 #pragma unroll
                     for (int half = 0; half < 2; ++half) qd[((w * SLABS + t) * 2 + half) * 64 + lane] = h[t][half];
             }
             __syncthreads();      // dU
-            const f32x4 then = beta;
-            if (c > 0) store(next);
-            load(max(c - 2, 0));
-            __syncthreads();      // Z
-            const f32x4 z = zf[w * 64 + lane];
-            float *Z = a.Z + ((first + (long long)c * a.Hv) * C + i0) * wide + x.dv0 + r16;
-            T *to = dV + (long long)(C * c + i0) * a.Hv * a.dv;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                Z[e * wide] = z[e];
-                if (there && i0 + e < len) to[(long long)e * a.Hv * a.dv] = (T)(now[e] * z[e]);
+            if (carry && c > 0) store(next);
+            if (LATER && read) {
+                if (c < last) put(c + 1);
+                now = next_rate, next_rate = rate_of;
             }
-            now = then;
+            if (carry) load(max(c - 2, 0));
+            __syncthreads();      // Z
+            if (!read) continue;
+            const float *q = zf + 4 * g * XP + t0;
+            z = f32x4{q[0], q[XP], q[2 * XP], q[3 * XP]};
+            if constexpr (!LATER) {
+                put(c);
+                now = rate_of;
+            }
             multiply(next);
             load_p(max(c - 2, 0));
             pd[w * 64 + lane] = p;
         }
+        if (LATER && read && last >= 0) put(0);
         return;
     }
 
@@ -485,14 +540,18 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(GDelta a)
     if (last >= 0) load_t(last);
     __syncthreads();
     __syncthreads();
+    Fragments<T, SLABS> kf, kc;
+    auto rows = [&](int c) { kf.template rows<KTile>(k_tile(c), K + (long long)C * c * a.kt, a.kt, len_of(c), a.dk, w, lane); };
+    auto cols = [&](int c) { kc.template cols<KTile>(k_tile(c), K + (long long)C * c * a.kt, a.kt, len_of(c), a.dk, w, lane); };
+    constexpr bool AHEAD = KTile::kBytes > 0;      // (as in the forward)
+    if (AHEAD && last >= 0 && holds) rows(last);
 
     for (int c = last; c >= 0; --c) {
-        const int len = len_of(c);
-        const T *Kc = k_tile(c), *Kg = K + (long long)C * c * a.kt;
+        if (!AHEAD && holds) rows(c);
         Of<T, 3> sp[SLABS];
 #pragma unroll
         for (int t = 0; t < SLABS; ++t) sp[t] = of<T, 3>(s[t]);
-        const f32x4 own = products<KTile, T, DK>(Kc, Kg, a.kt, len, a.dk, sp, parts, w, lane);
+        const f32x4 own = products<T, DK>(kf, sp, parts, w, lane);
         if (holds) put_state<true>(a.R + (first + (long long)c * a.Hv) * gdelta_state(a) + (x.dv0 + r16) * DK, k0, DK, s);
         __syncthreads();
 
@@ -500,27 +559,19 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(GDelta a)
         __syncthreads();
 
         f32x4 z = mma33(tf.f[1], Du.rows(r16, 32 + 8 * g), zero4());
-        if (w < 2) z = mma33(tf.f[0], Du.rows(r16, 8 * g), z);
+        if (w < 2) z += mma33(tf.f[0], Du.rows(r16, 8 * g), zero4());
         load_t(max(c - 1, 0));
         Zg.put4(r16, i0, z * *reinterpret_cast<const f32x4 *>(rate + (2 + (c & 1)) * C + i0));
-        zf[w * 64 + lane] = z;
+        *reinterpret_cast<f32x4 *>(zf + r16 * XP + i0) = z;
         const float all = rate[C + (c & 1)];
+        if (AHEAD && holds) cols(c);
         __syncthreads();
 
         if (holds) {
-#pragma unroll
-            for (int t = 0; t < SLABS; ++t) {
-                const f32x4 *q = qd + (w * SLABS + t) * 2 * 64 + lane;
-                f32x4 n[2] = {__builtin_shufflevector(s[t], s[t], 0, 1, 2, 3) * all + q[0], __builtin_shufflevector(s[t], s[t], 4, 5, 6, 7) * all + q[64]};
-#pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const Of<T, 3> zg = Zg.rows(r16, 32 * b + 8 * g);
-#pragma unroll
-                    for (int half = 0; half < 2; ++half)
-                        n[half] = mma<3>(KTile::cols8(Kc, Kg, a.kt, len, a.dk, 32 * b + 8 * g, 32 * (w * SLABS + t), half, r16), zg, n[half]);
-                }
-                s[t] = __builtin_shufflevector(n[0], n[1], 0, 1, 2, 3, 4, 5, 6, 7);
-            }
+            const Of<T, 3> zg[2] = {Zg.rows(r16, 8 * g), Zg.rows(r16, 32 + 8 * g)};
+            if (!AHEAD) cols(c);
+            else if (c > 0) rows(c - 1);
+            update<T, SLABS>(s, all, qd + w * SLABS * 128 + lane, kc, zg);
         }
     }
     if (a.dS0 && there && holds) put_state<FULL>(a.dS0 + (x.sh * a.dv + col) * a.dk, k0, a.dk, s);
@@ -528,24 +579,35 @@ __global__ __launch_bounds__(512) void scan_bwd_kernel(GDelta a)
 
 enum { kForward, kKeep, kBackward };
 
-template <typename T, int DK> hipError_t scan(const GDelta &a, bool full, int what, hipStream_t stream)
+template <typename T, int DK, bool FULL> void scan(const GDelta &a, int what, dim3 grid, hipStream_t stream)
+{
+    if (what == kForward) {
+        scan_kernel<T, DK, FULL, true><<<grid, 512, 0, stream>>>(a);
+    } else if (what == kKeep) {
+        scan_kernel<T, DK, FULL, false><<<grid, 512, 0, stream>>>(a);
+    } else {
+        // Backward: a third group of wavefronts where every workgroup has a compute unit for itself (2 x 8192 tokens, 16 heads of 128: 383 ->
+        // 373 us; of three groups no two workgroups have their registers there).  Wider or fp32: their values do not fit a third group's.
+        if constexpr (sizeof(T) == 2 && DK <= 128)
+            if (grid.x <= (unsigned)device_cu_count()) {
+                scan_bwd_kernel<T, DK, FULL, 3><<<grid, 768, 0, stream>>>(a);
+                return;
+            }
+        scan_bwd_kernel<T, DK, FULL, 2><<<grid, 512, 0, stream>>>(a);
+    }
+}
+template <typename T, int DK> hipError_t scan(const GDelta &a, int what, hipStream_t stream)
 {
     const int tiles = what == kForward ? (a.dv + N - 1) / N : (a.dv + 31) / 32 * 2;
     const double groups = (double)a.N * a.Hv * tiles;
-    if (!launch_holds(groups, 512)) return hipErrorInvalidConfiguration;
+    if (!launch_holds(groups, 768)) return hipErrorInvalidConfiguration;
     const dim3 grid((unsigned)groups);
-    if (what == kForward)
-        full ? scan_kernel<T, DK, true, true><<<grid, 512, 0, stream>>>(a) : scan_kernel<T, DK, false, true><<<grid, 512, 0, stream>>>(a);
-    else if (what == kKeep)
-        full ? scan_kernel<T, DK, true, false><<<grid, 512, 0, stream>>>(a) : scan_kernel<T, DK, false, false><<<grid, 512, 0, stream>>>(a);
-    else
-        full ? scan_bwd_kernel<T, DK, true><<<grid, 512, 0, stream>>>(a) : scan_bwd_kernel<T, DK, false><<<grid, 512, 0, stream>>>(a);
+    gdelta_full(a, sizeof(T)) ? scan<T, DK, true>(a, what, grid, stream) : scan<T, DK, false>(a, what, grid, stream);
     return hipGetLastError();
 }
 template <typename T> hipError_t scan(const GDelta &a, int what, hipStream_t stream)
 {
-    const bool full = gdelta_full(a, sizeof(T));
-    return a.dk <= 64 ? scan<T, 64>(a, full, what, stream) : a.dk <= 128 ? scan<T, 128>(a, full, what, stream) : scan<T, 256>(a, full, what, stream);
+    return a.dk <= 64 ? scan<T, 64>(a, what, stream) : a.dk <= 128 ? scan<T, 128>(a, what, stream) : scan<T, 256>(a, what, stream);
 }
 
 }  // namespace
