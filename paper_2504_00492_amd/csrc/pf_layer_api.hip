@@ -156,7 +156,7 @@ extern "C" pf_status pf_gated_bwd(const void *X, long long xb, long long xt, con
 
 extern "C" int pf_head_norm_supported(int d, int rot, pf_dtype dt)
 {
-    return known(dt) && d >= 1 && rot >= 0 && rot <= d && rot % 2 == 0 && d <= 8 * pf::kHeadUnits && pf::head_units(d, rot) <= pf::kHeadUnits;
+    return known(dt) && d >= 1 && rot >= 0 && rot <= d && rot % 2 == 0 && d <= 16 * pf::kHeadUnits && pf::head_units(d, rot) <= pf::kHeadUnits;
 }
 
 namespace {
@@ -197,7 +197,7 @@ extern "C" pf_status pf_head_norm_fwd(const void *Q, long long qt, long long qh,
 extern "C" size_t pf_head_norm_bwd_workspace_bytes(int M, int Hq, int Hk, int d, int rot)
 {
     if (M <= 0 || Hq < 0 || Hk < 0 || !pf_head_norm_supported(d, rot, PF_F32)) return 0;
-    return (size_t)pf::heads_bwd_parts(M, Hq, Hk, d, rot) * 2 * d * sizeof(float);
+    return (size_t)pf::heads_bwd_parts(M, Hq, Hk, d, rot) * d * sizeof(float);
 }
 
 extern "C" pf_status pf_head_norm_bwd(const void *Q, long long qt, long long qh, const void *K, long long kt, long long kh,

@@ -116,7 +116,7 @@ hipError_t launch_gdelta_step(const GDeltaStep &a, bool is_bf16, hipStream_t str
 
 // ---- norm and rotation of heads (pf_heads.hip)
 constexpr int kHeadUnits = 64;      // lanes that a row can take
-inline int head_units(int d, int rot) { return (rot / 2 + 3) / 4 + (d - rot + 7) / 8; }
+inline int head_units(int d, int rot) { return (rot / 2 + 7) / 8 + (d - rot + 15) / 16; }
 struct HeadSide {
     const void *X, *w, *dY;
     void *Y;                 // the output; of the backward: dX
@@ -129,7 +129,7 @@ struct Heads {
     HeadSide side[2];        // queries, keys
     const float *table;
     const int *positions;
-    float *part;             // backward: sums for dw, [2][heads_bwd_parts][d]
+    float *part;             // backward: sums for dw, [heads_bwd_parts][d]
     int M, d, rot, far, pairs, l2;
     float eps;
 };

@@ -68,6 +68,7 @@ SIZES = [
     (1, 1, 1, 128, 128), (4, 32, 32, 128, 128), (3, 4, 2, 64, 64), (17, 3, 1, 128, 64), (5, 2, 2, 72, 40), (33, 5, 3, 80, 80), (2, 1, 0, 16, 0),
     (7, 2, 1, 256, 256), (9, 3, 2, 256, 64), (3, 2, 1, 512, 512), (4, 1, 1, 504, 2), (6, 2, 2, 33, 10), (5, 1, 1, 1, 0), (8, 1, 2, 2, 2), (5, 3, 3, 20, 6),
     (1000, 6, 2, 128, 96), (300, 1, 1, 40, 24), (0, 2, 2, 64, 64),
+    (3, 2, 1, 1024, 1024), (2, 3, 1, 1010, 2), (5, 1, 1, 640, 256), (2, 70, 9, 32, 16), (3000, 1, 1, 16, 16),
 ]
 
 
@@ -121,6 +122,17 @@ def test_a_row_of_zeros_and_large_numbers(layer):
     assert not bool(Yq[0].any()) and bool((Yq[1] - 0.125).abs().max() <= 0.125 * 72 * 2.0 ** -24)
     dQ = layer.head_norm_bwd(Q, None, torch.ones_like(Q), None, norm="l2", eps=EPS)[0]
     assert bool(torch.isfinite(dQ).all()) and bool((dQ[0] - EPS ** -0.5).abs().max() <= 1e3 * 80 * 2.0 ** -24)
+
+
+def test_an_infinity_stays_in_its_place(layer):
+    """As the formula has it: NaN where the infinity lies and at its partner of a turn, zeros elsewhere."""
+    Q = torch.ones(3, 2, 96, device="cuda")
+    Q[1, 0, 90] = Q[2, 1, 5] = float("inf")
+    Yq, _ = layer.head_norm_fwd(Q, None, None, None, layer.rotary_table(10, 32), torch.arange(3, dtype=torch.int32, device="cuda"), norm="rms", eps=EPS)
+    nan = torch.zeros(3, 2, 96, dtype=torch.bool, device="cuda")
+    nan[1, 0, 90] = nan[2, 1, 5] = nan[2, 1, 5 + 16] = True
+    assert torch.equal(Yq.isnan(), nan)
+    assert not bool(Yq[1, 0][~nan[1, 0]].any()) and not bool(Yq[2, 1][~nan[2, 1]].any()) and bool((Yq[0] != 0).all())
 
 
 def test_in_place(layer):
