@@ -188,7 +188,7 @@ pf_status pf_gated_bwd(const void *X, long long xb, long long xt, const void *G,
  *   Yq, Yk     [M, Hq, d], [M, Hk, d]                      dt     out   Yq == Q, Yk == K is allowed where these are dense
  *
  * rot is even, from 0 to d.  ceil(rot / 16) + ceil((d - rot) / 16) up to 64 (pf_head_norm_supported; else PF_ERR_UNSUPPORTED): d up to 1010 at
- * least, 1024 where 16 divides rot.  M == 0: nothing is done.  Squares are summed in fp32 (as in pf_norm_fwd).
+ * least, 1024 where 16 divides rot.  Hq + Hk up to 2^24.  M == 0: nothing is done.  Squares are summed in fp32 (as in pf_norm_fwd).
  */
 typedef enum { PF_NORM_RMS = 0, PF_NORM_L2 = 1 } pf_norm_kind;
 

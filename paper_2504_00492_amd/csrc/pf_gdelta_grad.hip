@@ -61,17 +61,33 @@ __global__ __launch_bounds__(256) void grad_kernel(GDelta a)
 #pragma unroll
     for (int n = 0; n < 4; ++n) X[n] = Y[n] = kk[n] = zero4();
     float zv = 0.f;
+    struct {
+        In<T> o, v;
+        f32x8 z;
+        f32x4 u[C * ROWS / 4 / 256];
+    } next;      // the next step's loads, asked for a step ahead
+    auto ask = [&](int v0) {
+        next.o = o_at(v0 + 8 * g), next.v = fetch<T, false>(V + v0 + 8 * g, a.dv - v0 - 8 * g);
+        next.z = *reinterpret_cast<const f32x8 *>(Z + v0 + 8 * g);
+#pragma unroll
+        for (int i = 0; i < C * ROWS / 4 / 256; ++i) {
+            const int at = i * 256 + threadIdx.x;
+            next.u[i] = *reinterpret_cast<const f32x4 *>(U + at / (ROWS / 4) * wide + v0 + 4 * (at % (ROWS / 4)));
+        }
+    };
+    ask(0);
     for (int v0 = 0; v0 < wide; v0 += ROWS) {
-        const In<T> of_o = o_at(v0 + 8 * g);
-        const f32x8 z = *reinterpret_cast<const f32x8 *>(Z + v0 + 8 * g), v = in_f32(fetch<T, false>(V + v0 + 8 * g, a.dv - v0 - 8 * g));
+        const In<T> of_o = next.o;
+        const f32x8 z = next.z, v = in_f32(next.v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) zv += z[e] * v[e];
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < C * ROWS / 4 / 256; ++i) {
-            const int at = i * 256 + threadIdx.x, row = at / (ROWS / 4), k = 4 * (at % (ROWS / 4));
-            Us.put4(row, k, *reinterpret_cast<const f32x4 *>(U + row * wide + v0 + k));
+            const int at = i * 256 + threadIdx.x;
+            Us.put4(at / (ROWS / 4), 4 * (at % (ROWS / 4)), next.u[i]);
         }
+        ask(min(v0 + ROWS, wide - ROWS));
         __syncthreads();
         const Of<T, 2> of_z = of<T, 2>(z);
 #pragma unroll
@@ -82,10 +98,20 @@ __global__ __launch_bounds__(256) void grad_kernel(GDelta a)
         }
     }
     zv = sum_of_groups(zv);      // of token 16 w + r16
-    for (int k = 8 * g; k < DK; k += 32) {
-        const In<T> ka = fetch<T, FULL>(K + mine * a.kt + k, a.dk - k);
+    In<T> kn[5];
+    auto keys = [&](int k) {
+        kn[4] = fetch<T, FULL>(K + mine * a.kt + k, a.dk - k);
 #pragma unroll
-        for (int n = 0; n < 4; ++n) kk[n] = mma(ka, fetch<T, FULL>(K + min(16 * n + r16, x.len - 1) * a.kt + k, a.dk - k), kk[n]);
+        for (int n = 0; n < 4; ++n) kn[n] = fetch<T, FULL>(K + min(16 * n + r16, x.len - 1) * a.kt + k, a.dk - k);
+    };
+    keys(8 * g);
+    for (int k = 8 * g; k < DK; k += 32) {
+        In<T> now[5];
+#pragma unroll
+        for (int n = 0; n < 5; ++n) now[n] = kn[n];
+        keys(min(k + 32, DK - 32 + 8 * g));
+#pragma unroll
+        for (int n = 0; n < 4; ++n) kk[n] = mma(now[4], now[n], kk[n]);
     }
     const bf16 *Pt = a.P + xi * kMatrix;      // of the transpose, in three parts
     f32x4 row = zero4(), yk = zero4();
@@ -123,33 +149,59 @@ __global__ __launch_bounds__(256) void grad_kernel(GDelta a)
     // ---- 64 columns of dQ and dK at a time
     f32x4 oq = zero4(), uk = zero4(), zk = zero4();
     float dot = 0.f;
+    constexpr int NS = ROWS * COLS / 4 / 256, NK = C * COLS / 8 / 256;
+    struct {
+        In<T> o;
+        f32x8 u, z;
+        f32x4 s[NS], r[NS];
+    } step;      // the next step's, and the next columns of K and Q
+    In<T> kr[NK], qr[NK];
+    auto states = [&](int c0, int v0) {
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            const int at = i * 256 + threadIdx.x, from = (v0 + at / (COLS / 4)) * DK + c0 + 4 * (at % (COLS / 4));
+            step.s[i] = *reinterpret_cast<const f32x4 *>(S + from), step.r[i] = *reinterpret_cast<const f32x4 *>(R + from);
+        }
+        step.o = o_at(v0 + 8 * g);
+        step.u = *reinterpret_cast<const f32x8 *>(U + (16 * w + r16) * wide + v0 + 8 * g);
+        step.z = *reinterpret_cast<const f32x8 *>(Z + v0 + 8 * g);
+    };
+    auto columns = [&](int c0) {
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            const int at = i * 256 + threadIdx.x, from = min(at / (COLS / 8), x.len - 1), k = c0 + 8 * (at % (COLS / 8));
+            kr[i] = fetch<T, FULL>(K + from * a.kt + k, a.dk - k), qr[i] = fetch<T, FULL>(Q + from * a.qt + k, a.dk - k);
+        }
+    };
+    columns(0);
+    states(0, 0);
     for (int c0 = 0; c0 < DK; c0 += COLS) {
         f32x4 oS[NC], uR[NC], zS[NC];
 #pragma unroll
         for (int n = 0; n < NC; ++n) oS[n] = uR[n] = zS[n] = zero4();
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            const int at = i * 256 + threadIdx.x, to = at / (COLS / 8) * KP + 8 * (at % (COLS / 8));
+            __builtin_memcpy(__builtin_assume_aligned(Ks + to, 16), &kr[i], sizeof(kr[i]));
+            __builtin_memcpy(__builtin_assume_aligned(Qs + to, 16), &qr[i], sizeof(qr[i]));
+        }
+        const int behind = min(c0 + COLS, DK - COLS);
+        columns(behind);
         for (int v0 = 0; v0 < wide; v0 += ROWS) {
-            const In<T> of_o = o_at(v0 + 8 * g);
-            const f32x8 u = *reinterpret_cast<const f32x8 *>(U + (16 * w + r16) * wide + v0 + 8 * g);
-            const f32x8 z = *reinterpret_cast<const f32x8 *>(Z + v0 + 8 * g);
+            const In<T> of_o = step.o;
+            const f32x8 u = step.u, z = step.z;
             __syncthreads();
-            if (v0 == 0) {
 #pragma unroll
-                for (int i = 0; i < C * COLS / 8 / 256; ++i) {
-                    const int at = i * 256 + threadIdx.x, r = at / (COLS / 8), k = 8 * (at % (COLS / 8)), from = min(r, x.len - 1);
-                    const In<T> kr = fetch<T, FULL>(K + from * a.kt + c0 + k, a.dk - c0 - k), qr = fetch<T, FULL>(Q + from * a.qt + c0 + k, a.dk - c0 - k);
-                    __builtin_memcpy(__builtin_assume_aligned(Ks + r * KP + k, 16), &kr, sizeof(kr));
-                    __builtin_memcpy(__builtin_assume_aligned(Qs + r * KP + k, 16), &qr, sizeof(qr));
-                }
+            for (int i = 0; i < NS; ++i) {
+                const int at = i * 256 + threadIdx.x, r = at / (COLS / 4), k = 4 * (at % (COLS / 4));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dot += step.s[i][e] * step.r[i][e];
+                Ss.put4(r, k, step.s[i]);
+                Rs.put4(r, k, step.r[i]);
             }
-#pragma unroll
-            for (int i = 0; i < ROWS * COLS / 4 / 256; ++i) {
-                const int at = i * 256 + threadIdx.x, r = at / (COLS / 4), k = 4 * (at % (COLS / 4)), from = (v0 + r) * DK + c0 + k;
-                const f32x4 sv = *reinterpret_cast<const f32x4 *>(S + from), rv = *reinterpret_cast<const f32x4 *>(R + from);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) dot += sv[e] * rv[e];
-                Ss.put4(r, k, sv);
-                Rs.put4(r, k, rv);
-            }
+            const bool over = v0 + ROWS >= wide;
+            states(over ? behind : c0, over ? 0 : v0 + ROWS);
             __syncthreads();
             const Of<T, 2> of_z = of<T, 2>(z), of_u = of<T, 2>(u);
 #pragma unroll

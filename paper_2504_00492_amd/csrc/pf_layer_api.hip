@@ -166,6 +166,7 @@ pf_status heads_checks(const pf::Heads &a, bool backward, pf_norm_kind kind, pf_
     if (a.M < 0 || a.d <= 0 || a.rot < 0 || a.rot > a.d || a.rot % 2) return PF_ERR_SHAPE;
     if (a.side[0].H < 0 || a.side[1].H < 0 || a.far < 0) return PF_ERR_SHAPE;
     if (!pf_head_norm_supported(a.d, a.rot, dt) || (kind != PF_NORM_RMS && kind != PF_NORM_L2)) return PF_ERR_UNSUPPORTED;
+    if ((long long)a.side[0].H + a.side[1].H > pf::kHeadsMost) return PF_ERR_UNSUPPORTED;
     const bool rows = a.M > 0;
     if (rows && a.rot && (!a.table || !a.positions)) return PF_ERR_NULL;
     for (const pf::HeadSide &s : a.side) {
@@ -196,7 +197,7 @@ extern "C" pf_status pf_head_norm_fwd(const void *Q, long long qt, long long qh,
 
 extern "C" size_t pf_head_norm_bwd_workspace_bytes(int M, int Hq, int Hk, int d, int rot)
 {
-    if (M <= 0 || Hq < 0 || Hk < 0 || !pf_head_norm_supported(d, rot, PF_F32)) return 0;
+    if (M <= 0 || Hq < 0 || Hk < 0 || (long long)Hq + Hk > pf::kHeadsMost || !pf_head_norm_supported(d, rot, PF_F32)) return 0;
     return (size_t)pf::heads_bwd_parts(M, Hq, Hk, d, rot) * d * sizeof(float);
 }
 

@@ -116,6 +116,7 @@ hipError_t launch_gdelta_step(const GDeltaStep &a, bool is_bf16, hipStream_t str
 
 // ---- norm and rotation of heads (pf_heads.hip)
 constexpr int kHeadUnits = 64;      // lanes that a row can take
+constexpr int kHeadsMost = 1 << 24; // heads of a token, queries and keys (counted in 32 bits)
 inline int head_units(int d, int rot) { return (rot / 2 + 7) / 8 + (d - rot + 15) / 16; }
 struct HeadSide {
     const void *X, *w, *dY;
