@@ -1,0 +1,159 @@
+"""The norm of heads with rotation and the gated delta rule run together: the example's third half against the same in plain operations, prompts
+against tokens and packed sequences, its gradients against automatic ones; and the two operators one behind the other in float32, forward and
+backward, eager and captured.
+
+Bars of the example: an 8-bit rounding is off by 2^-4 of a value at most, 2.7 % of it in the mean square, and a product of two such
+operands by 3.8 % of its norm; a branch goes through two products (5.4 %), what the recurrence makes of the first not counted: 0.12 leaves a
+factor of two.  Gradients go through the incoming gradient's product, the recurrence's inputs (products of the same kind) and the
+weights' product: three to four of 3.8 %, 7.6 %, and 0.2 leaves more than a factor of two.  Between two ways over the same roundings only some 8-bit roundings
+fall otherwise: 0.05, as a whole product's error is 3.8 %."""
+import pytest
+import torch
+
+import gated_delta_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ex():
+    from paper_2504_00492_amd import example_layer
+    return example_layer
+
+
+def rel(a, b):
+    return float((a.double() - b.double()).norm() / b.double().norm())
+
+
+def norm(x, w):
+    return x / (x.square().mean(-1, keepdim=True) + 1e-5).sqrt() * w
+
+
+def plain(ex, w, x, tokens, at, leaves):
+    """x [M, D] and leaves (weights by name) in float64."""
+    H, Hk, d = w.heads, w.keys, w.d
+    p = (norm(x, leaves["norm_keys"]) @ leaves["qkvgb"].t()).view(-1, 2 * Hk * d + H * d + 2 * H)
+    q, k, v, g, b = p.split([Hk * d, Hk * d, H * d, H, H], 1)
+    q, k = (ref.heads(t.reshape(-1, Hk, d), leaves[n], w.table, at, "l2", ex.EPS, s, False) for t, n, s in ((q, "norm_q", d ** -0.5), (k, "norm_k", 1.0)))
+    rows = lambda t, *s: t.reshape(-1, tokens, *s)  # noqa: E731
+    o, S = ref.delta(rows(q, Hk, d), rows(k, Hk, d), rows(v, H, d), rows(-torch.nn.functional.softplus(g + w.bias_decay), H), rows(b.sigmoid(), H))
+    return norm(o.reshape(-1, d), leaves["norm_values"]).reshape(-1, H * d) @ leaves["out_keys"].t(), S
+
+
+def weights_of(w):
+    named = dict(norm_keys=w.norm_keys, norm_q=w.norm_q, norm_k=w.norm_k, norm_values=w.norm_values, qkvgb=w.plain["qkvgb"], out_keys=w.plain["out_keys"])
+    return {k: t.double().requires_grad_() for k, t in named.items()}
+
+
+@pytest.mark.parametrize("heads", [4, 3])
+def test_prompt_and_gradients_against_plain_operations(ex, heads):
+    B, tokens, w = 2, 90, ex.Weights(heads=heads, d=64, r=1, seed=heads, training=True)
+    gen = torch.Generator().manual_seed(8)
+    x, dy, ds = (torch.randn((B * tokens, w.width), generator=gen).cuda().bfloat16() for _ in range(3))
+    at = (torch.arange(tokens).repeat(B) + 100).int().cuda()
+    keep = {}
+    stream, branch, last = ex.keys_half(w, x, None, None, tokens, at, keep=keep)
+    leaves = weights_of(w)
+    X = x.double().requires_grad_()
+    want, S = plain(ex, w, X, tokens, at, leaves)
+    assert torch.equal(stream, x) and rel(branch, want.detach()) < 0.12 and rel(last, S.detach()) < 0.12
+    d_x, grads = ex.keys_half_backward(w, keep, dy, ds)
+    assert set(grads) == set(leaves)
+    auto = torch.autograd.grad((want * dy.double()).sum() + (X * ds.double()).sum(), [X, *leaves.values()])
+    for name, got, ref_grad in zip(("x", *leaves), (d_x, *(grads[k] for k in leaves)), auto):
+        assert rel(got, ref_grad) < 0.2, name
+
+
+def test_token_by_token_is_the_prompt(ex):
+    B, tokens, w = 3, 70, ex.Weights(heads=2, d=64, r=1, seed=5)
+    x = torch.randn((B, tokens, w.width), generator=torch.Generator().manual_seed(6)).cuda().bfloat16()
+    at = torch.arange(tokens, dtype=torch.int32, device="cuda")
+    _, whole, last = ex.keys_half(w, x.view(-1, w.width), None, None, tokens, at.repeat(B))
+    pool, slots = torch.zeros(6, 2, 64, 64, device="cuda"), torch.tensor([4, 0, 3], dtype=torch.int32, device="cuda")
+    outs = [ex.keys_half(w, x[:, t].contiguous(), None, pool, 1, at[t].repeat(B), slots=slots)[1] for t in range(tokens)]
+    assert rel(torch.stack(outs, 1).view_as(whole), whole) < 0.05
+    assert rel(pool[slots.long()], last) < 0.05 and not bool(pool[[1, 2, 5]].any())
+    # and a prompt's state goes on token by token
+    _, _, first = ex.keys_half(w, x[:, :50].reshape(-1, w.width), None, None, 50, at[:50].repeat(B))
+    pool[slots.long()] = first
+    outs = [ex.keys_half(w, x[:, t].contiguous(), None, pool, 1, at[t].repeat(B), slots=slots)[1] for t in range(50, tokens)]
+    assert rel(torch.stack(outs, 1), whole.view(B, tokens, -1)[:, 50:]) < 0.05
+
+
+def test_packed_is_each_by_itself(ex):
+    w, ends = ex.Weights(heads=2, d=64, r=1, seed=9), [0, 7, 7, 100, 230]
+    x = torch.randn((230, w.width), generator=torch.Generator().manual_seed(10)).cuda().bfloat16()
+    at = torch.cat([torch.arange(b - a) for a, b in zip(ends, ends[1:])]).int().cuda()
+    _, whole, last = ex.keys_half(w, x, None, None, 0, at, offsets=torch.tensor(ends, dtype=torch.int32).cuda())
+    for n, (a, b) in enumerate(zip(ends, ends[1:])):
+        if b > a:
+            _, one, state = ex.keys_half(w, x[a:b], None, None, b - a, at[a:b])
+            assert rel(whole[a:b], one) < 0.05 and rel(last[n:n + 1], state) < 0.05
+        else:
+            assert not bool(last[n].any())
+
+
+def chain(layer, Q, K, V, G, beta, wq, wk, table, at, dO):
+    """Forward and backward of the two operators, whole sequences [B, L]."""
+    how = dict(norm="l2", eps=1e-6, q_scale=0.125)
+    lead = V.shape[:2]
+    q, k = layer.head_norm_fwd(Q, K, wq, wk, table, at, **how)
+    inputs = (q.unflatten(0, lead), k.unflatten(0, lead), V, G, beta)
+    O, S = layer.gated_delta_fwd(*inputs)
+    dq, dk, dV, dG, db, _ = layer.gated_delta_bwd(*inputs, dO)
+    dQ, dK, dwq, dwk = layer.head_norm_bwd(Q, K, dq.flatten(0, 1), dk.flatten(0, 1), wq, wk, table, at, **how)
+    return O, S, dQ, dK, dV, dG, db, dwq, dwk
+
+
+def chain_inputs(layer, B, L, Hk, Hv, d, dt):
+    g = torch.Generator().manual_seed(L)
+    n = lambda *s: torch.randn(s, generator=g).to(dt).cuda()  # noqa: E731
+    Q, K, V, dO = n(B * L, Hk, d), n(B * L, Hk, d), n(B, L, Hv, d), n(B, L, Hv, d)
+    G, beta = -torch.nn.functional.softplus(n(B, L, Hv)), n(B, L, Hv).sigmoid()
+    wq, wk = 1 + n(d) * 0.1, 1 + n(d) * 0.1
+    return Q, K, V, G, beta, wq, wk, layer.rotary_table(L, d // 2), torch.arange(L).repeat(B).int().cuda(), dO
+
+
+def test_chain_in_float32(ex):
+    """Tolerance: the gated delta rule's own, 2 (d + 128) 2^-24, and a norm's (d + 8) 2^-24 in front of it and one behind, each of which it may make
+    larger: a key's error enters a token's change twice, and what it leaves in the state fades with the gates, by a half a token here in the mean, so four times at
+    most: eight in all."""
+    layer = ex.layer
+    args = chain_inputs(layer, 2, 150, 2, 4, 64, torch.float32)
+    got = chain(layer, *args)
+    Q, K, V, G, beta, wq, wk = leaves = [t.double().cpu().requires_grad_() for t in args[:7]]
+    table, at, dO = (t.cpu() for t in args[7:])
+    q, k = (ref.heads(t, w, table, at, "l2", 1e-6, s, False).unflatten(0, (2, 150)) for t, w, s in ((Q, wq, 0.125), (K, wk, 1.0)))
+    O, S = ref.delta(q, k, V, G, beta)
+    want = (O.detach(), S.detach(), *torch.autograd.grad((O * dO.double()).sum(), leaves))
+    for i, (a, b) in enumerate(zip(got, want)):
+        off = ref.off(a.cpu(), b)
+        assert off <= 2 * (64 + 128) * 2.0 ** -24 + 16 * (64 + 8) * 2.0 ** -24, (i, off)
+
+
+def test_chain_captured(ex):
+    """Captured while an eager run's outputs live, replayed with other inputs, eager work between: the eager run's bits every time."""
+    layer = ex.layer
+    args = chain_inputs(layer, 2, 150, 2, 4, 64, torch.bfloat16)
+    chain(layer, *args)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        chain(layer, *args)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = chain(layer, *args)
+    for turn in range(4):
+        args[0].mul_(0.75).add_(0.1 * turn)
+        args[3].mul_(0.9)
+        graph.replay()
+        want = chain(layer, *args)
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b)
+
+
+def test_main_runs(ex, capsys):
+    ex.main()
+    assert "gated delta rule, prompt against token by token" in capsys.readouterr().out
