@@ -268,7 +268,7 @@ pf_status pf_gated_delta_fwd(const void *Q, long long qb, long long qt, long lon
  *   dV        [N, L, Hv, d_v]                              dt     out
  *   dG, dbeta [N, L, Hv]                                   dt     out
  *   dS0       [N, Hv, d_v, d_k]                            fp32   out   NULL: not written.  dS0 == dSL is allowed
- *   workspace / workspace_bytes                            ..., backward = 1: for every 64 tokens and head of 128 x 128 about 230 KB
+ *   workspace / workspace_bytes                            ..., backward = 1: for every 64 tokens and head of 128 x 128 about 250 KB
  */
 pf_status pf_gated_delta_bwd(const void *Q, long long qb, long long qt, long long qh, const void *K, long long kb, long long kt,
                              long long kh, const void *V, long long vb, long long vt, long long vh, const void *G, long long gb,

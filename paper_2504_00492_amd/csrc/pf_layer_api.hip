@@ -230,10 +230,10 @@ pf_status gdelta_sizes(pf::GDelta &a, pf_dtype dt)
 {
     if (a.N < 0 || a.L < 0 || a.Hk <= 0 || a.Hv <= 0 || a.dk <= 0 || a.dv <= 0 || a.Hv % a.Hk) return PF_ERR_SHAPE;
     if (a.L > 1 << 30 || !gdelta_known(a.Hk, a.Hv, a.dk, a.dv, dt)) return PF_ERR_UNSUPPORTED;
-    // chunks, and threads of the kernels that have a workgroup for each of them and a head, are counted in 32 bits
+    // chunks, and threads of the kernels that have a workgroup for each of them and a head, or for 16 rows of a sequence's state, are counted in 32 bits
     const long long C = pf::kGDeltaChunk, some = a.N < a.L ? a.N : a.L;
     const long long per = (a.L + C - 1) / C, chunks = a.offsets ? (a.L + (C - 1) * some) / C : per * a.N;
-    if (!pf::launch_holds((double)chunks * a.Hv, 512) || !pf::launch_holds((double)a.N * a.Hv, 256)) return PF_ERR_UNSUPPORTED;
+    if (!pf::launch_holds((double)chunks * a.Hv, 512) || !pf::launch_holds((double)a.N * a.Hv * ((a.dv + 31) / 32 * 2), 768)) return PF_ERR_UNSUPPORTED;
     a.per = (int)per, a.chunks = (int)chunks;
     a.rows = a.offsets ? 0 : a.L;
     if (a.offsets) a.qb = a.kb = a.vb = a.gb = a.bb = a.ob = 0;      // (all in one row of tokens)

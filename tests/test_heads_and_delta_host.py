@@ -88,7 +88,7 @@ def test_refusals(layer, call, wrong, status):  # noqa: F811
 
 @pytest.mark.parametrize("call,sizes", [
     (_delta_fwd, dict(N=1, L=(1 << 30) + 1)), (_delta_bwd, dict(N=1, L=BIG)), (_delta_fwd, dict(N=1 << 24, L=64, Hk=1, Hv=1)),
-    (_delta_fwd, dict(N=BIG, L=0, Hk=1, Hv=1)), (_delta_bwd, dict(N=1 << 20, L=1024, Hk=1, Hv=1)), (_delta_fwd, dict(N=BIG, L=1 << 30, Hk=1, Hv=1, offsets=P)),
+    (_delta_fwd, dict(N=BIG, L=0, Hk=1, Hv=1)), (_delta_fwd, dict(N=1 << 19, L=1, Hk=1, Hv=1, dv=256)), (_delta_bwd, dict(N=1 << 16, L=1, Hk=1, Hv=8, dv=250)), (_delta_bwd, dict(N=1 << 20, L=1024, Hk=1, Hv=1)), (_delta_fwd, dict(N=BIG, L=1 << 30, Hk=1, Hv=1, offsets=P)),
     (_delta_bwd, dict(N=1, L=64, Hk=1, Hv=1 << 24)), (_delta_step, dict(B=1 << 24, pool=1 << 24, Hk=1, Hv=1)), (_delta_step, dict(B=BIG, pool=BIG)),
     (_delta_step, dict(B=1, pool=1, Hk=1, Hv=BIG)), (_heads_fwd, dict(M=BIG, Hq=1 << 23)), (_heads_fwd, dict(M=BIG, Hq=64, Hk=64, d=1024, rot=0))])
 def test_more_than_a_launch_holds(layer, call, sizes):  # noqa: F811
