@@ -261,6 +261,12 @@ size_t gdelta_workspace(GDelta &a, bool backward, void *at)
     part(a.vec, x * gd::kVec);
     part(a.T, x * gd::kMatrix);
     part(a.P, x * gd::kMatrix);
+    if (a.segments > 1) {
+        const size_t each = (size_t)a.N * a.Hv * a.segments * gdelta_width(a.dk);
+        part(a.ends, each * (dv + gdelta_width(a.dk)));
+        part(a.starts, each * dv);
+        if (backward) part(a.fronts, each * dv);
+    }
     if (backward) {
         part(a.Tt, x * gd::kMatrix);
         part(a.S, x * gdelta_state(a));

@@ -97,20 +97,25 @@ template <int NP, bool LOW> struct Pairs {
     }
 };
 
-struct Place {      // of a workgroup: its sequence, head and first row of the state
-    int seq, h, hk, dv0, chunks;
+struct Place {      // of a workgroup: its sequence, head and first row of the state; its segment, whose tokens and chunks q has
+    int seq, h, hk, dv0, chunks, seg;
     Sequence q;
-    long long sh;
+    long long sh, at;      // at: of the segment among all
 };
 __device__ __forceinline__ Place place_of(const GDelta &a, int tiles)
 {
     // tiles of one head side by side, on one XCD: they read the same K, Q, T and P
     Place x;
-    const int id = uniform((int)xcd_consecutive(blockIdx.x, gridDim.x)), sh = id / tiles;
-    x.sh = sh;
-    x.seq = sh / a.Hv, x.h = sh - x.seq * a.Hv, x.hk = x.h / (a.Hv / a.Hk), x.dv0 = (id - sh * tiles) * N;
+    const int id = uniform((int)xcd_consecutive(blockIdx.x, gridDim.x)), all = id / tiles, sh = all / a.segments;
+    x.sh = sh, x.at = all, x.seg = all - sh * a.segments;
+    x.seq = sh / a.Hv, x.h = sh - x.seq * a.Hv, x.hk = x.h / (a.Hv / a.Hk), x.dv0 = (id - all * tiles) * N;
     x.q = sequence_at(a, x.seq);
     x.chunks = (x.q.len + C - 1) / C;
+    if (a.segments > 1) {
+        const int from = (int)((long long)x.chunks * x.seg / a.segments), to = (int)((long long)x.chunks * (x.seg + 1) / a.segments);
+        x.q = {x.q.tok + C * from, min(x.q.len, C * to) - C * from, x.q.first + from};
+        x.chunks = to - from;
+    }
     return x;
 }
 __device__ __forceinline__ int wide_of(const GDelta &a) { return (a.dv + 31) / 32 * 32; }
@@ -206,10 +211,14 @@ template <typename T> __device__ __forceinline__ void put_row(T *to, f32x4 v, in
     }
 }
 
-// Forward.  OUT: O is wanted; else the states before every chunk and U are kept for the backward.
-template <typename T, int DK, bool FULL, bool OUT>
+enum { kForward, kKeep, kEnds, kBackward };
+
+// Forward.  kForward: O is wanted; kKeep: the states before every chunk and U are kept for the backward; kEnds: the states behind each segment alone,
+// from zeros, and in d_k more rows what a segment makes of the unit matrix (with no values).
+template <typename T, int DK, bool FULL, int WHAT>
 __global__ __launch_bounds__(512) void scan_kernel(GDelta a)
 {
+    constexpr bool OUT = WHAT == kForward;
     constexpr int KS = DK / 32, NPO = sizeof(T) == 2 ? 2 : 3, SLABS = Share<DK>::SLABS, UP = C + 4;      // NPO: parts on the way into O
     typedef Tile<T, NPO, N, DK> StateTile;
     typedef Tile<T, 3, N, C> LaterTile;
@@ -227,7 +236,7 @@ __global__ __launch_bounds__(512) void scan_kernel(GDelta a)
     const StateTile Sp = {reinterpret_cast<T *>(at)};
     auto k_tile = [&](int c) { return reinterpret_cast<T *>(smem + (c & 1) * KTile::kBytes); };
 
-    const Place x = place_of(a, OUT ? (a.dv + N - 1) / N : wide_of(a) / N);
+    const Place x = place_of(a, OUT ? (a.dv + N - 1) / N : (wide_of(a) + (WHAT == kEnds ? DK : 0)) / N);
     const int w = wave_id() & 3, lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4, i0 = 16 * w + 4 * g;
     const int col = min(x.dv0 + r16, a.dv - 1);      // this lane's row of the state; those behind d_v are zeros
     const bool there = x.dv0 + r16 < a.dv;
@@ -310,7 +319,7 @@ __global__ __launch_bounds__(512) void scan_kernel(GDelta a)
                 if (w >= 2) o[0] = mma_parts<NPO>(u(1), pf.f[1], o[0]);
                 load_p(next);
                 if (t0 < len_of(c) && left > 0) put_row(O + (long long)C * c * a.Hv * a.dv, o[0] + o[1], left, whole);
-            } else {
+            } else if constexpr (WHAT == kKeep) {
                 const float *u = Uf + 4 * g * UP + t0;
                 *reinterpret_cast<f32x4 *>(a.U + ((first + (long long)c * a.Hv) * C + t0) * wide + x.dv0 + 4 * g) = f32x4{u[0], u[UP], u[2 * UP], u[3 * UP]};
             }
@@ -324,7 +333,17 @@ __global__ __launch_bounds__(512) void scan_kernel(GDelta a)
     f32x8 s[SLABS];
 #pragma unroll
     for (int t = 0; t < SLABS; ++t) s[t] = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (a.S0 && there && holds) get_state<FULL>(a.S0 + (x.sh * a.dv + col) * a.dk, k0, a.dk, s);
+    const int wide = wide_of(a);
+    if constexpr (WHAT == kEnds) {
+#pragma unroll
+        for (int t = 0; t < SLABS; ++t)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[t][e] = x.dv0 + r16 == wide + k0 + 32 * t + e ? 1.f : 0.f;
+    } else if (a.segments > 1) {
+        if (holds) get_state<true>(a.starts + (x.at * wide + x.dv0 + r16) * DK, k0, DK, s);
+    } else if (a.S0 && there && holds) {
+        get_state<FULL>(a.S0 + (x.sh * a.dv + col) * a.dk, k0, a.dk, s);
+    }
     Pairs<3, true> tf;
     auto load_t = [&](int c) { tf.load(a.T + (first + (long long)c * a.Hv) * kMatrix, w, lane); };
     if (x.chunks > 0) load_t(0);
@@ -345,7 +364,7 @@ __global__ __launch_bounds__(512) void scan_kernel(GDelta a)
             if constexpr (OUT) {
 #pragma unroll
                 for (int t = 0; t < SLABS; ++t) Sp.put8(r16, k0 + 32 * t, sp[t]);
-            } else {
+            } else if constexpr (WHAT == kKeep) {
                 put_state<true>(a.S + (first + (long long)c * a.Hv) * gdelta_state(a) + (x.dv0 + r16) * DK, k0, DK, s);
             }
         }
@@ -371,14 +390,16 @@ __global__ __launch_bounds__(512) void scan_kernel(GDelta a)
             update<T, SLABS>(s, all, nullptr, kc, ud);
         }
     }
-    if (OUT && a.SL && there && holds) put_state<FULL>(a.SL + (x.sh * a.dv + col) * a.dk, k0, a.dk, s);
+    if (WHAT == kEnds && holds) put_state<true>(a.ends + (x.at * (wide + DK) + x.dv0 + r16) * DK, k0, DK, s);
+    if (OUT && a.SL && there && holds && x.seg == a.segments - 1) put_state<FULL>(a.SL + (x.sh * a.dv + col) * a.dk, k0, a.dk, s);
 }
 
 // Backward, from the last chunk to the first, with R the gradient of the state behind a chunk:
 //   dU = P^T dO + delta K R^T ,  Z = T^T dU ,  dV = beta Z ,  R' = gamma_64 R + (gamma dO)^T Q - (gamma beta Z)^T K .
+// ends: R in front of each segment alone, from zeros (what else is written is written again behind that).
 // R and Z are kept for the gradients of Q, K and the gates.  P^T dO and (gamma dO)^T Q are computed beside the chain, a chunk ahead.
 template <typename T, int DK, bool FULL, int GROUPS>
-__global__ __launch_bounds__(256 * GROUPS) void scan_bwd_kernel(GDelta a)
+__global__ __launch_bounds__(256 * GROUPS) void scan_bwd_kernel(GDelta a, bool ends)
 {
     constexpr int OP = pitch<T>(C), XP = C + 4, SLABS = Share<DK>::SLABS, HOLDERS = Share<DK>::HOLDERS;
     typedef Tile<T, 3, N, C> TokenTile;
@@ -537,7 +558,11 @@ __global__ __launch_bounds__(256 * GROUPS) void scan_bwd_kernel(GDelta a)
     f32x8 s[SLABS];
 #pragma unroll
     for (int t = 0; t < SLABS; ++t) s[t] = f32x8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (a.dSL && there && holds) get_state<FULL>(a.dSL + (x.sh * a.dv + col) * a.dk, k0, a.dk, s);
+    if (a.segments > 1) {
+        if (holds && !ends) get_state<true>(a.starts + (x.at * wide + x.dv0 + r16) * DK, k0, DK, s);
+    } else if (a.dSL && there && holds) {
+        get_state<FULL>(a.dSL + (x.sh * a.dv + col) * a.dk, k0, a.dk, s);
+    }
     Pairs<3, false> tf;
     auto load_t = [&](int c) { tf.load(a.Tt + (first + (long long)c * a.Hv) * kMatrix, w, lane); };
     if (last >= 0) load_t(last);
@@ -577,34 +602,109 @@ __global__ __launch_bounds__(256 * GROUPS) void scan_bwd_kernel(GDelta a)
             update<T, SLABS>(s, all, qd + w * SLABS * 128 + lane, kc, zg);
         }
     }
-    if (a.dS0 && there && holds) put_state<FULL>(a.dS0 + (x.sh * a.dv + col) * a.dk, k0, a.dk, s);
+    if (ends) {
+        if (holds) put_state<true>(a.fronts + (x.at * wide + x.dv0 + r16) * DK, k0, DK, s);
+    } else if (a.dS0 && there && holds && x.seg == 0) {
+        put_state<FULL>(a.dS0 + (x.sh * a.dv + col) * a.dk, k0, a.dk, s);
+    }
 }
 
-enum { kForward, kKeep, kBackward };
+// States at the ends of segments, one segment after the other, S <- S M + L with M what the segment makes of the unit matrix and L its state from
+// zeros; BACK: gradients, from the last on, R <- R M^T + L.  A workgroup has 16 rows of a state, a wavefront 16 columns of it; a step's M is asked
+// for a step ahead.
+template <int DK, bool BACK> __global__ __launch_bounds__(4 * DK) void join_kernel(GDelta a)
+{
+    constexpr int STEPS = DK / 4, P = DK + 4;
+    __shared__ __attribute__((aligned(16))) float state[2][16 * P];
+    const int wide = wide_of(a), tiles = wide / N, w = wave_id(), lane = threadIdx.x & 63, r16 = lane & 15, g = lane >> 4;
+    const long long sh = blockIdx.x / tiles;
+    const int dv0 = (int)(blockIdx.x - sh * tiles) * N, col = 16 * w + r16;
+    const float *first = BACK ? a.dSL : a.S0;
+    f32x4 s;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int row = dv0 + 4 * g + e;
+        s[e] = first && row < a.dv && col < a.dk ? first[(sh * a.dv + row) * a.dk + col] : 0.f;
+    }
+    f32x4 m[STEPS / 4];      // of its column, every fourth row from g on (BACK: of M^T the rows from STEPS g on, in whole vectors)
+    f32x4 l;
+    const uint32_t mine = g * DK + col;      // (beside an address that is the same for all lanes)
+    auto ask = [&](int seg) {
+        const long long at = sh * a.segments + seg;
+        const float *M = a.ends + (at * (wide + DK) + wide) * DK, *L = BACK ? a.fronts + (at * wide + dv0 + 4 * g) * DK + col : a.ends + (at * (wide + DK) + dv0 + 4 * g) * DK + col;
+#pragma unroll
+        for (int i = 0; i < STEPS / 4; ++i) {
+            if constexpr (BACK) m[i] = *reinterpret_cast<const f32x4 *>(M + col * DK + STEPS * g + 4 * i);
+            else
+#pragma unroll
+                for (int e = 0; e < 4; ++e) m[i][e] = (M + 4 * (4 * i + e) * DK)[mine];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) l[e] = L[e * DK];
+    };
+    ask(BACK ? a.segments - 1 : 0);
+    for (int i = 0; i < a.segments; ++i) {
+        const int seg = BACK ? a.segments - 1 - i : i;
+        float *now = state[i & 1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            a.starts[((sh * a.segments + seg) * wide + dv0 + 4 * g + e) * DK + col] = s[e];
+            now[(4 * g + e) * P + col] = s[e];
+        }
+        __syncthreads();
+        f32x4 n[2] = {l, zero4()};
+#pragma unroll
+        for (int i = 0; i < STEPS / 4; ++i) {
+            f32x4 x;
+            if constexpr (BACK) x = *reinterpret_cast<const f32x4 *>(now + r16 * P + STEPS * g + 4 * i);
+            else
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = now[r16 * P + 4 * (4 * i + e) + g];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) n[e & 1] = mfma4(x[e], m[i][e], n[e & 1]);
+        }
+        s = n[0] + n[1];
+        const int next = BACK ? seg - 1 : seg + 1;
+        ask(min(max(next, 0), a.segments - 1));
+    }
+}
 
-template <typename T, int DK, bool FULL> void scan(const GDelta &a, int what, dim3 grid, hipStream_t stream)
+template <typename T, int DK, bool FULL> void scan(const GDelta &a, int what, bool ends, dim3 grid, hipStream_t stream)
 {
     if (what == kForward) {
-        scan_kernel<T, DK, FULL, true><<<grid, 512, 0, stream>>>(a);
+        scan_kernel<T, DK, FULL, kForward><<<grid, 512, 0, stream>>>(a);
     } else if (what == kKeep) {
-        scan_kernel<T, DK, FULL, false><<<grid, 512, 0, stream>>>(a);
+        scan_kernel<T, DK, FULL, kKeep><<<grid, 512, 0, stream>>>(a);
+    } else if (what == kEnds) {
+        scan_kernel<T, DK, FULL, kEnds><<<grid, 512, 0, stream>>>(a);
     } else {
         // Backward: a third group of wavefronts where every workgroup has a compute unit for itself (2 x 8192 tokens, 16 heads of 128: 383 ->
         // 373 us; of three groups no two workgroups have their registers there).  Wider or fp32: their values do not fit a third group's.
         if constexpr (sizeof(T) == 2 && DK <= 128)
             if (grid.x <= (unsigned)device_cu_count()) {
-                scan_bwd_kernel<T, DK, FULL, 3><<<grid, 768, 0, stream>>>(a);
+                scan_bwd_kernel<T, DK, FULL, 3><<<grid, 768, 0, stream>>>(a, ends);
                 return;
             }
-        scan_bwd_kernel<T, DK, FULL, 2><<<grid, 512, 0, stream>>>(a);
+        scan_bwd_kernel<T, DK, FULL, 2><<<grid, 512, 0, stream>>>(a, ends);
     }
 }
 template <typename T, int DK> hipError_t scan(const GDelta &a, int what, hipStream_t stream)
 {
-    const int tiles = what == kForward ? (a.dv + N - 1) / N : (a.dv + 31) / 32 * 2;
-    const dim3 grid((unsigned)((long long)a.N * a.Hv * tiles));
-    gdelta_full(a, sizeof(T)) ? scan<T, DK, true>(a, what, grid, stream) : scan<T, DK, false>(a, what, grid, stream);
-    return hipGetLastError();
+    const bool full = gdelta_full(a, sizeof(T));
+    const int wide = (a.dv + 31) / 32 * 32;
+    auto run = [&](int how, bool ends) {
+        const int rows = how == kForward ? a.dv : how == kEnds ? wide + DK : wide;
+        const dim3 grid((unsigned)((long long)a.N * a.Hv * a.segments * ((rows + N - 1) / N)));
+        full ? scan<T, DK, true>(a, how, ends, grid, stream) : scan<T, DK, false>(a, how, ends, grid, stream);
+        return hipGetLastError();
+    };
+    if (a.segments > 1) {
+        const dim3 grid((unsigned)((long long)a.N * a.Hv * (wide / N)));
+        if (hipError_t e = run(what == kBackward ? kBackward : kEnds, what == kBackward)) return e;
+        what == kBackward ? join_kernel<DK, true><<<grid, 4 * DK, 0, stream>>>(a) : join_kernel<DK, false><<<grid, 4 * DK, 0, stream>>>(a);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    return run(what, false);
 }
 template <typename T> hipError_t scan(const GDelta &a, int what, hipStream_t stream)
 {

@@ -235,6 +235,7 @@ pf_status gdelta_sizes(pf::GDelta &a, pf_dtype dt)
     const long long per = (a.L + C - 1) / C, chunks = a.offsets ? (a.L + (C - 1) * some) / C : per * a.N;
     if (!pf::launch_holds((double)chunks * a.Hv, 512) || !pf::launch_holds((double)a.N * a.Hv * ((a.dv + 31) / 32 * 2), 768)) return PF_ERR_UNSUPPORTED;
     a.per = (int)per, a.chunks = (int)chunks;
+    a.segments = pf::gdelta_segments(a);
     a.rows = a.offsets ? 0 : a.L;
     if (a.offsets) a.qb = a.kb = a.vb = a.gb = a.bb = a.ob = 0;      // (all in one row of tokens)
     return PF_OK;

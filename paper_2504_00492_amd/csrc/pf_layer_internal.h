@@ -83,6 +83,8 @@ struct GDelta {
     int *plan;               // the workspace's parts, set by gdelta_workspace
     __bf16 *T, *P, *Tt;      // Tt: backward
     float *vec, *S, *U, *Z, *R;
+    float *ends, *starts, *fronts;      // of segments: states from zeros and of the unit matrix; states they start from; gradients from zeros
+    int segments;            // of a sequence, run side by side (1: none are cut)
 };
 // d_k is padded with zeros to a width that the kernels have
 __host__ __device__ inline int gdelta_width(int dk) { return dk <= 64 ? 64 : dk <= 128 ? 128 : 256; }
@@ -93,6 +95,21 @@ inline bool gdelta_full(const GDelta &a, int size)
 {
     const uintptr_t all = reinterpret_cast<uintptr_t>(a.Q) | reinterpret_cast<uintptr_t>(a.K) | (uintptr_t)((a.qb | a.qt | a.qh | a.kb | a.kt | a.kh) * size);
     return a.dk == gdelta_width(a.dk) && all % 16 == 0;
+}
+// Segments that sequences are cut into, where their chains are few: each is run twice, the first time with as many rows more as the state has
+// columns, and what joins them takes them one after the other.  Of that first run two workgroups to a compute unit at most, eight chunks to a
+// segment at least, and no more segments than make a step of the join (1.7 us) worth the chunks (1.5 us, twice) that it saves; it pays from three
+// segments and 32 chunks on.  bf16, heads of 128, forward, cut and whole: 65536 tokens of one head 215 and 1554 us, of four 586 and 1893, of eight
+// 1122 and 2009; 2048 tokens of one head 49 and 63, 1600 in three segments 51 and 51 (their backward 138 and 121).
+inline int gdelta_segments(const GDelta &a)
+{
+    if (a.chunks == 0 || a.N == 0) return 1;
+    const double chains = (double)a.N * a.Hv * ((a.dv + 31) / 32 * 32 + gdelta_width(a.dk)) / 16;
+    const int chunks = a.chunks / a.N;
+    int n = chains < 512 ? (int)(512 / chains) : 1;
+    n = n < chunks / 8 ? n : chunks / 8;
+    while (n > 1 && 2ll * n * n > 3ll * chunks) --n;
+    return n < 3 || chunks < 32 ? 1 : n;
 }
 // Bytes of the workspace; a's parts of it, where `at` is not NULL.
 size_t gdelta_workspace(GDelta &a, bool backward, void *at);

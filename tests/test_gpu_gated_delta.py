@@ -99,6 +99,24 @@ def test_packed_sequences(layer, lengths, behind, dtype):
     check(layer, args, S0, dO, dSL, dt, 64, off, ends)
 
 
+@pytest.mark.parametrize("gate", [1.0, 0.01])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", [(1, 1600, 1, 1, 64, 64), (1, 2000, 1, 2, 128, 128), (2, 1700, 1, 1, 72, 40), (1, 1537, 1, 1, 256, 130), (1, 4100, 1, 1, 128, 16),
+                                  (3, 0, 1, 1, 64, 48)], ids=lambda s: "x".join(map(str, s)))
+def test_few_long_sequences(layer, size, dtype, gate, monkeypatch):
+    """Cut into segments that run side by side.  To what a chunk adds come the errors of what a segment makes of the unit matrix, of the same size, and
+    the d_k rounded products of joining them: three times F32 in all.  The last size: packed ones, one of them empty, one shorter than a segment."""
+    monkeypatch.setitem(globals(), "f32_bound", lambda dk: 6 * (dk + 128) * 2.0 ** -24)
+    B, L, *heads = size
+    if L:
+        args, S0, dO, dSL = make(B, L, *heads, DT[dtype], seed=sum(size), gate=gate)
+        check(layer, args, S0, dO, dSL, DT[dtype], heads[2])
+    else:
+        ends = [3, 2603, 2603, 2643]
+        args, S0, dO, dSL = make(B, 0, *heads, DT[dtype], seed=sum(size), gate=gate, rows=(1, 2650))
+        check(layer, args, S0, dO, dSL, DT[dtype], heads[2], torch.tensor(ends, dtype=torch.int32).cuda(), ends)
+
+
 def test_rows_of_no_sequence_are_left_alone(layer):
     args, S0, dO, dSL = make(2, 0, 1, 2, 64, 48, torch.bfloat16, rows=(1, 100))
     for t in (*args, dO):
