@@ -339,3 +339,71 @@ def test_a_workspace_with_anything_in_it(layer):
     ws = torch.full((need // 4,), float("nan"), device="cuda")
     for a, b in zip(layer.gated_delta_bwd(*args, dO, S0, dSL, workspace=ws), want):
         assert torch.equal(a, b)
+
+
+def test_segments_in_place_captured_and_with_anything_in_the_workspace(layer):
+    """One long sequence, cut: S_L in the place of S0 and dS0 in that of dS_L, NaN in the workspaces, captured, on another stream, slices of a projection:
+    the same bits always."""
+    sizes = (1, 2500, 1, 2, 64, 64)
+    args, S0, dO, dSL = make(*sizes, torch.bfloat16, gate=0.1)
+    want = (*layer.gated_delta_fwd(*args, S0), *layer.gated_delta_bwd(*args, dO, S0, dSL))
+    wide = torch.zeros(1, 2500, 1024, dtype=torch.bfloat16, device="cuda")
+    low, parts = 8, []
+    for t in args:
+        n = t[0, 0].numel()
+        wide[..., low:low + n] = t.flatten(2)
+        parts.append(wide[..., low:low + n].unflatten(2, t.shape[2:]))
+        low += n
+    ws = [torch.full((layer.pf_gated_delta_workspace_bytes(*sizes, 0, b, layer.PF_BF16) // 4,), float("nan"), device="cuda") for b in (0, 1)]
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    others = [(*layer.gated_delta_fwd(*parts, S0, workspace=ws[0]), *layer.gated_delta_bwd(*parts, dO, S0, dSL, workspace=ws[1])),
+              (*layer.gated_delta_fwd(*args, S0, stream=s), *layer.gated_delta_bwd(*args, dO, S0, dSL, stream=s))]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        others.append((*layer.gated_delta_fwd(*args, S0), *layer.gated_delta_bwd(*args, dO, S0, dSL)))
+    for _ in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        for got in others:
+            for a, b in zip(got, want):
+                assert torch.equal(a, b)
+        others[2][0].zero_(), others[2][2].zero_()
+    graph.replay()
+    arrays = [x for t in args for x in (t, *t.stride()[:3])]
+    stream = torch.cuda.current_stream().cuda_stream
+    S, R, O = S0.clone(), dSL.clone(), torch.empty_like(want[0])
+    assert layer.pf_gated_delta_fwd(*arrays, S, None, O, S, *sizes, layer.PF_BF16, ws[0], 4 * ws[0].numel(), stream) == 0
+    grads = [torch.empty_like(t) for t in want[2:7]]
+    assert layer.pf_gated_delta_bwd(*arrays, dO, *dO.stride()[:3], S0, R, None, *grads, R, *sizes, layer.PF_BF16, ws[1], 4 * ws[1].numel(), stream) == 0
+    for a, b in zip((O, S, *grads, R), want):
+        assert torch.equal(a, b)
+
+
+def test_offsets_beyond_32_bits(layer):
+    """Rows that lie 120 KB apart, 4.8 GB in all, and a pool of 9 GB: the same bits as dense ones."""
+    L, W = 40000, 60000
+    args, _, dO, _ = make(1, L, 1, 2, 64, 64, torch.bfloat16, s0=False)
+    wide = torch.empty(1, L, W, dtype=torch.bfloat16, device="cuda")
+    low, parts = W - 1024, []
+    for t in (*args, dO):
+        n = t[0, 0].numel()
+        wide[..., low:low + n] = t.flatten(2)
+        parts.append(wide[..., low:low + n].unflatten(2, t.shape[2:]))
+        low += n + -n % 8
+    for a, b in zip(layer.gated_delta_fwd(*parts[:5]), layer.gated_delta_fwd(*args)):
+        assert torch.equal(a, b)
+    for a, b in zip(layer.gated_delta_bwd(*parts), layer.gated_delta_bwd(*args, dO)):
+        assert torch.equal(a, b)
+    table, at = layer.rotary_table(L, 64), torch.arange(L, dtype=torch.int32, device="cuda")
+    for a, b in zip(layer.head_norm_fwd(parts[0][0], parts[1][0], None, None, table, at, norm="l2", eps=1e-6),
+                    layer.head_norm_fwd(args[0][0], args[1][0], None, None, table, at, norm="l2", eps=1e-6)):
+        assert torch.equal(a, b)
+    del wide, parts
+    pool = torch.zeros(2150, 64, 128, 128, device="cuda")
+    (Q, K, V, G, beta), S0, _, _ = make(3, 1, 64, 64, 128, 128, torch.bfloat16)
+    tokens, slots = [t[:, 0] for t in (Q, K, V, G, beta)], torch.tensor([2149, 0, 2148], dtype=torch.int32).cuda()
+    pool[slots.long()] = S0
+    O = layer.gated_delta_step(*tokens, pool, slots)
+    assert torch.equal(O, layer.gated_delta_step(*tokens, S0)) and torch.equal(pool[slots.long()], S0) and not bool(pool[1:2148].any())
