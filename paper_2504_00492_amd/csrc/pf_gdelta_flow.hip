@@ -17,13 +17,13 @@ __global__ __launch_bounds__(1024) void plan_kernel(GDelta a)
     if (t == 0) carry[0] = carry[1] = 0;
     __syncthreads();
     for (int base = 0; base < a.N; base += 1024) {
-        const int n = base + t;
+        const int n = base + t, span = min(1024, a.N - base);
         auto offset = [&](int i) { return i <= a.N ? min(max(a.offsets[i], 0), a.L) : 0; };
         // the largest offset up to n: a running maximum, side by side
         int best = n < a.N ? offset(n) : 0;
         smem[0][t] = best;
         __syncthreads();
-        for (int s = 1; s < 1024; s *= 2) {
+        for (int s = 1; s < span; s *= 2) {
             const int other = t >= s ? smem[0][t - s] : 0;
             __syncthreads();
             best = max(best, other);
@@ -36,7 +36,7 @@ __global__ __launch_bounds__(1024) void plan_kernel(GDelta a)
         int sum = mine;
         smem[1][t] = sum;
         __syncthreads();
-        for (int s = 1; s < 1024; s *= 2) {
+        for (int s = 1; s < span; s *= 2) {
             const int other = t >= s ? smem[1][t - s] : 0;
             __syncthreads();
             sum += other;
@@ -45,7 +45,7 @@ __global__ __launch_bounds__(1024) void plan_kernel(GDelta a)
         }
         if (n < a.N) p.start[n] = start, p.len[n] = len, p.first[n] = carry[1] + sum - mine;
         __syncthreads();
-        if (t == 1023) carry[0] = max(carry[0], best), carry[1] += sum;
+        if (t == span - 1) carry[0] = max(carry[0], best), carry[1] += sum;
         __syncthreads();
     }
     const int there = carry[1];

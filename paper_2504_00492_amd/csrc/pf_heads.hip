@@ -213,39 +213,30 @@ __global__ __launch_bounds__(256) void heads_bwd_kernel(Heads a, int parts0, int
     }
 }
 
-// dw out of the workgroups' parts: 16 columns to a workgroup, four threads of four columns times 64 rows
-__global__ __launch_bounds__(256) void heads_sum_kernel(Heads a, int parts0, int parts)
+// dw out of the workgroups' parts: 16 columns to a workgroup, 64 rows of them side by side
+__global__ __launch_bounds__(1024) void heads_sum_kernel(Heads a, int parts0, int parts)
 {
-    __shared__ float sums[64][20];
-    const int k = blockIdx.y, n = k ? parts - parts0 : parts0, col = blockIdx.x * 16 + 4 * (threadIdx.x & 3), r = threadIdx.x >> 2;
+    __shared__ float sums[64][17];
+    const int k = blockIdx.y, n = k ? parts - parts0 : parts0, col = blockIdx.x * 16 + (threadIdx.x & 15), r = threadIdx.x >> 4;
     float *dw = a.side[k].dw;
     if (!dw) return;
-    const float *p = a.part + (long long)(k ? parts0 : 0) * a.d + col;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    const float *p = a.part + (long long)(k ? parts0 : 0) * a.d + min(col, a.d - 1);
+    float sum = 0.f;
     int i = r;
     for (; i + 3 * 64 < n; i += 4 * 64) {      // (four loads under way together)
-        float v[4][4];
+        float v[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[j][e] = col + e < a.d ? p[(long long)(i + 64 * j) * a.d + e] : 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum[e] += v[j][e];
+        for (int j = 0; j < 4; ++j) v[j] = p[(long long)(i + 64 * j) * a.d];
+        sum += (v[0] + v[1]) + (v[2] + v[3]);
     }
-    for (; i < n; i += 64)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += col + e < a.d ? p[(long long)i * a.d + e] : 0.f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sums[r][4 * (threadIdx.x & 3) + e] = sum[e];
+    for (; i < n; i += 64) sum += p[(long long)i * a.d];
+    sums[r][threadIdx.x & 15] = sum;
     __syncthreads();
-    const int at = blockIdx.x * 16 + threadIdx.x;
-    if (threadIdx.x < 16 && at < a.d) {
+    if (threadIdx.x < 16 && col < a.d) {
         float all = 0.f;
 #pragma unroll
         for (int j = 0; j < 64; ++j) all += sums[j][threadIdx.x];
-        dw[at] = all;
+        dw[col] = all;
     }
 }
 
@@ -308,7 +299,7 @@ template <typename T, int LPR> hipError_t backward(const Heads &a, hipStream_t s
         dw ? heads_bwd_kernel<T, LPR, false, true><<<n.all, 256, 0, stream>>>(a, n.queries, n.each)
            : heads_bwd_kernel<T, LPR, false, false><<<n.all, 256, 0, stream>>>(a, n.queries, n.each);
     if (hipError_t e = hipGetLastError()) return e;
-    if (dw) heads_sum_kernel<<<dim3((a.d + 15) / 16, 2), 256, 0, stream>>>(a, n.queries, n.all);
+    if (dw) heads_sum_kernel<<<dim3((a.d + 15) / 16, 2), 1024, 0, stream>>>(a, n.queries, n.all);
     return hipGetLastError();
 }
 template <typename T> hipError_t heads(const Heads &a, bool back, hipStream_t stream)
