@@ -1,6 +1,6 @@
 // Norm of every head of queries and keys with the rotation by the token's position, and its backward (include/pf_layer.h).  Memory
 // is what bounds both: a row is read once and written once (the backward reads two).  65536 tokens of 64 heads of 128 in bf16, 1.07 GB each
-// way: 405 us, 5.3 TB/s (a copy of that size 423); the backward of 16383 tokens of 48 such heads 124 us, 4.9 TB/s.  (With units of eight values,
+// way: 405 us, 5.3 TB/s (a copy of that size 423); the backward of 16383 tokens of 48 such heads 122 us, 5.0 TB/s.  (With units of eight values,
 // so of 8-byte accesses, and four rows of a lane under way: 575 and 193.)
 //
 // A row of d values is cut into units of sixteen for a lane, two pieces of eight: of the turned ones eight pairs, a and b of a pair in the same

@@ -157,3 +157,36 @@ def test_chain_captured(ex):
 def test_main_runs(ex, capsys):
     ex.main()
     assert "gated delta rule, prompt against token by token" in capsys.readouterr().out
+
+
+def test_refusals_of_tensors(ex):
+    """Said before any call: another type, shape, order, place or number of an argument; and the library's own refusals as PfError."""
+    from paper_2504_00492_amd.binding import PfError
+    layer = ex.layer
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt, device="cuda")  # noqa: E731
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    Q, V, g, S = z(2, 5, 2, 16), z(2, 5, 4, 8), z(2, 5, 4), z(2, 4, 8, 16, dt=torch.float32)
+    fwd, bwd, step = layer.gated_delta_fwd, layer.gated_delta_bwd, layer.gated_delta_step
+    heads, back = layer.head_norm_fwd, layer.head_norm_bwd
+    q, v, b = Q[:, 0], V[:, 0], g[:, 0]
+    t, at = layer.rotary_table(9, 8), i32(0, 1)
+    for call in (lambda: fwd(Q, Q.float(), V, g, g), lambda: fwd(Q, Q[:, :4], V, g, g), lambda: fwd(Q, Q, V[..., 0], g, g), lambda: fwd(Q, Q, V[:, :, :3], g[..., :3], g[..., :3]),
+                 lambda: fwd(Q, Q, V, g.float(), g), lambda: fwd(Q, Q, V, g, g[..., :1]), lambda: fwd(Q, Q, V, g, g, S[:1]), lambda: fwd(Q, Q, V, g, g, S.bfloat16()),
+                 lambda: fwd(Q, Q, V, g, g, S.transpose(0, 1)), lambda: fwd(Q.transpose(2, 3).contiguous().transpose(2, 3), Q, V, g, g), lambda: fwd(Q.half(), Q, V, g, g),
+                 lambda: fwd(Q, Q.cpu(), V, g, g), lambda: fwd(Q, Q, V, g, g, offsets=i32(0, 5, 10)), lambda: fwd(Q[:1], Q[:1], V[:1], g[:1], g[:1], offsets=i32(0, 5).long()),
+                 lambda: fwd(Q[:1], Q[:1], V[:1], g[:1], g[:1], offsets=i32(0, 5).cpu()), lambda: fwd(Q[:1], Q[:1], V[:1], g[:1], g[:1], offsets=i32()),
+                 lambda: fwd(Q, Q, V, g, g, workspace=torch.zeros(1 << 20)), lambda: bwd(Q, Q, V, g, g, V[:, :3]), lambda: bwd(Q, Q, V, g, g, V, S, S[:1]),
+                 lambda: step(q, q, v, b, b, S[:1]), lambda: step(q, q, v, b, b, S, i32(0)), lambda: step(q, q, v, b, b, S, i32(0, 1).long()), lambda: step(q, q, v, b, b, S[..., :15]),
+                 lambda: step(q, q, v, b, b, S.bfloat16()), lambda: step(q, q, v, b[:1], b, S), lambda: step(Q, Q, V, g, g, S),
+                 lambda: heads(q, q[:1], eps=0.0), lambda: heads(q, None, None, z(16), eps=0.0), lambda: heads(q, q, z(15), eps=0.0), lambda: heads(q, q, z(16).float(), eps=0.0),
+                 lambda: heads(q, q, None, None, t, eps=0.0), lambda: heads(q, q, None, None, None, at, eps=0.0), lambda: heads(q, q, None, None, t, at.long(), eps=0.0),
+                 lambda: heads(q, q, None, None, t[:, :7], at, eps=0.0), lambda: heads(q, q, None, None, layer.rotary_table(9, 18), at, eps=0.0), lambda: heads(q, q, norm="l1", eps=0.0),
+                 lambda: heads(q, q, None, None, t.bfloat16(), at, eps=0.0), lambda: back(q, q, q, None, eps=0.0), lambda: back(q, None, q, q, eps=0.0), lambda: back(q, q, q[:1], q, eps=0.0)):
+        with pytest.raises(ValueError):
+            call()
+    small = torch.zeros(16, dtype=torch.uint8, device="cuda")
+    for call in (lambda: fwd(z(1, 3, 1, 257), z(1, 3, 1, 257), z(1, 3, 1, 8), z(1, 3, 1), z(1, 3, 1)), lambda: fwd(Q, Q, V, g, g, workspace=small),
+                 lambda: bwd(Q, Q, V, g, g, V, workspace=small), lambda: back(q, q, q, q, z(16), eps=0.0, workspace=small), lambda: heads(z(2, 1, 1025), eps=0.0),
+                 lambda: fwd(Q, Q, V, g, g, torch.zeros(2 * 4 * 8 * 16 + 1, device="cuda")[1:].view(2, 4, 8, 16))):
+        with pytest.raises(PfError):
+            call()
