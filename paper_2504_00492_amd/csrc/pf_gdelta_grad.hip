@@ -4,9 +4,11 @@
 //   dQ = gamma dO S + (D X) K                      X on and below the diagonal, Y below it
 //   dK = (D X)^T Q + W K + W^T K + delta U R - beta gamma Z S ,   W = beta D Y
 //   dbeta_i = z_i.v_i - gamma_i z_i.S k_i + sum over j of Y_ij D_ij k_i.k_j
-//   dg_t = sum over i >= t of e_i  +  <R, S'> ,   <R, S'> = gamma_64 <R, S> + sum of delta_j u_j.R k_j ,
-//   e_i  = gamma_i do_i.S q_i - delta_i u_i.R k_i - beta_i gamma_i z_i.S k_i
-//          + sum over j < i of (X P + Y A)_ij - sum over j > i of (X P + Y A)_ji .
+//   dg_t = sum over i >= t > j of M_ij + sum over i >= t of (gamma_i do_i.S q_i - beta_i gamma_i z_i.S k_i)
+//          + sum over j < t of delta_j u_j.R k_j + gamma_64 <R, S> ,   M = X P + Y A .
+//
+// Every term of dg_t is of what goes from tokens before t, or the state, to t and later ones, or the next state, so it has t's gate in it.  (As
+// differences of sums over whole rows and columns of M the same cost 2e-5 of the gradient at gates of -5, all of it at -16.)
 #include "pf_gdelta.h"
 
 namespace pf {
@@ -41,7 +43,7 @@ __global__ __launch_bounds__(512) void grad_kernel(GDelta a)
     __shared__ __attribute__((aligned(16))) char states[2][StateTile::kBytes], values[UTile::kBytes], tokens[2][kTokens], pairs[2][PairTile::kBytes];
     __shared__ __attribute__((aligned(16))) float rows[3][C];      // gamma, delta, beta
     __shared__ float coarse[C], fine[C];
-    __shared__ float srow[2][C], sbeta[2][C], scol[4][C], sdot[8];
+    __shared__ float srow[2][C], sstate[2][C], slater[2][C], sbeta[2][C], scol[4][C], sdot[8];
     const StateTile Ss = {reinterpret_cast<T *>(states[0])}, Rs = {reinterpret_cast<T *>(states[1])};
     const UTile Us = {reinterpret_cast<T *>(values)};
     T *Ks = reinterpret_cast<T *>(tokens[0]), *Qs = reinterpret_cast<T *>(tokens[1]);
@@ -182,7 +184,7 @@ __global__ __launch_bounds__(512) void grad_kernel(GDelta a)
                 for (int m = 0; m < NP; ++m) kk[m] = mma(ka, frag_rows(Ks, KP, 16 * (2 * m + half) + r16, k), kk[m]);
             }
             for (int k = COLS + 8 * g; k < DK; k += 32) {
-                const In<T> ka = fetch<T, FULL>(K + mine * a.kt + k, a.dk - k);
+                const In<T> ka = fetch<T, FULL>(K + min(16 * w + r16, x.len - 1) * a.kt + k, a.dk - k);
 #pragma unroll
                 for (int m = 0; m < NP; ++m) kk[m] = mma(ka, fetch<T, FULL>(K + min(16 * (2 * m + half) + r16, x.len - 1) * a.kt + k, a.dk - k), kk[m]);
             }
@@ -191,14 +193,15 @@ __global__ __launch_bounds__(512) void grad_kernel(GDelta a)
                 const f32x4 beta = ld_rows(2);
                 const int n = 2 * m + half, j = 16 * n + r16;
                 f32x4 w1 = zero4(), w2 = zero4();
-                float col = 0.f;
                 if (n <= w) {
                     const float cj = coarse[j], fj = fine[j];
                     f32x4 p = zero4();
 #pragma unroll
                     for (int q = 2; q >= 0; --q) p += __builtin_convertvector(pt[m][q], f32x4);
+                    f32x4 below;      // of column j's M: from row i on
+                    float sum = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
+                    for (int e = 3; e >= 0; --e) {
                         const int i = i0 + e;
                         const float D = power(coarse[i] - cj, fine[i] - fj);
                         const bool in = i < x.len;
@@ -206,15 +209,16 @@ __global__ __launch_bounds__(512) void grad_kernel(GDelta a)
                         const float y = in && j < i ? -Y[m][e] * D : 0.f;
                         w2[e] = beta[e] * y;
                         yk[e] += y * kk[m][e];
-                        const float both = (in && j < i ? X[m][e] * p[e] : 0.f) + w2[e] * kk[m][e];
-                        row[e] += both;
-                        col += both;
+                        below[e] = sum += (in && j < i ? X[m][e] * p[e] : 0.f) + w2[e] * kk[m][e];
                     }
+                    const float near = __shfl_xor(sum, 16), far = __shfl_xor(sum + near, 32);
+                    below += (g & 1 ? 0.f : near) + (g & 2 ? 0.f : far);      // (groups behind)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) row[e] += j < i0 + e ? below[e] : 0.f;
+                    if (g == 0) scol[w][j] = sum + near + far;
                 }
                 W1.put4(j, i0, w1);
                 W2.put4(j, i0, w2);
-                col = sum_of_groups(col);
-                if (g == 0) scol[w][j] = col;
             }
             __syncthreads();
             again();
@@ -285,22 +289,34 @@ __global__ __launch_bounds__(512) void grad_kernel(GDelta a)
         row[e] = sum_of_16(row[e]), yk[e] = sum_of_16(yk[e]);
         const float zvi = half == 0 ? __shfl(zv, 4 * g + e) : 0.f;
         if (r16 == 0) {
-            srow[half][i0 + e] = oq[e] - uk[e] - beta[e] * zk[e] + row[e];
+            srow[half][i0 + e] = row[e];
+            sstate[half][i0 + e] = oq[e] - beta[e] * zk[e];
+            slater[half][i0 + e] = uk[e];
             sbeta[half][i0 + e] = zvi - zk[e] + yk[e];
         }
     }
-    {      // <R, S'>: every wavefront's part of gamma_64 <R, S>, and of its tokens' delta u.R k (none behind the end, where u = 0)
-        const float sum = sum_of_groups(uk[0] + uk[1] + uk[2] + uk[3]);
-        dot = sum_of_groups(sum_of_16(dot));
-        if (lane == 0) sdot[wave_id()] = vec.gamma[C - 1] * dot + sum;
-    }
+    dot = sum_of_groups(sum_of_16(dot));
+    if (lane == 0) sdot[wave_id()] = vec.gamma[C - 1] * dot;
     __syncthreads();
-    if (wave_id() == 0) {      // sums from the chunk's end
-        float e = lane < x.len ? srow[0][lane] + srow[1][lane] - (scol[0][lane] + scol[1][lane] + scol[2][lane] + scol[3][lane]) : 0.f;
+    if (wave_id() == 0) {      // sums up to the chunk's end, and of the tokens before: u.R k, and M's of each later 16 rows
+        float after = lane < x.len ? sstate[0][lane] + sstate[1][lane] : 0.f, before[4] = {slater[0][lane] + slater[1][lane]};
+#pragma unroll
+        for (int b = 1; b < 4; ++b) before[b] = lane < 16 * b ? scol[b][lane] : 0.f;
 #pragma unroll
         for (int s = 1; s < 64; s *= 2) {
-            const float other = __shfl_down(e, s);
-            if (lane + s < 64) e += other;
+            const float other = __shfl_down(after, s);
+            if (lane + s < 64) after += other;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const float other = __shfl_up(before[b], s);
+                if (lane >= s) before[b] += other;
+            }
+        }
+        float e = after + srow[0][lane] + srow[1][lane];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const float sum = __shfl_up(before[b], 1);
+            if (lane > 0 && (b == 0 || lane < 16 * b)) e += sum;
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) e += sdot[i];

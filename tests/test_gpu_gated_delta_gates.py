@@ -1,0 +1,51 @@
+"""Gradients of the gated delta rule where its gates are strong, head by head against the definition in 64 bits.
+
+The gradient of a token's log gate is a_t <R_t', S_{t-1}>: what reaches a later token, or the state behind, from an earlier one or the state
+before, so it has the gate for a factor and is as small.  Tolerances are those of test_gpu_gated_delta, of each head's own gradients, since
+every term of the sums carries that factor and none is a difference of larger ones: (d_k + 128) rounded sums and as much again in
+fp32, and for bf16 the output's rounding and four operands of 16 bits."""
+import pytest
+import torch
+
+import gated_delta_ref as ref
+from test_gpu_gated_delta import DT, bound, layer, make, wide  # noqa: F401  (layer: fixture)
+
+pytestmark = pytest.mark.gpu
+
+GATES = (-0.1, -2.0, -5.0, -8.0, -12.0, -16.0, -30.0, -60.0)
+
+
+def by_heads(layer, args, S0, dO, dSL, dk):  # noqa: F811
+    got = layer.gated_delta_bwd(*args, dO, S0, dSL)
+    want = ref.delta_grads(wide(*args, S0), *wide(dO, dSL))
+    for name, a, b in zip(("dV", "dG", "dbeta"), got[2:5], want[2:5]):
+        for h in range(b.shape[2]):
+            tol, off = bound(a.dtype, dk), ref.off(a[:, :, h], b[:, :, h])
+            assert off <= tol, (name, h, off, tol)
+    return got
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("L,Hk,dk,dv", [(64, 8, 64, 64), (130, 4, 128, 32), (70, 8, 72, 40), (150, 2, 256, 64), (2100, 1, 64, 32)])
+def test_each_head_a_gate_of_its_own(layer, L, Hk, dk, dv, dtype):  # noqa: F811
+    """The last size in segments: two of the gates at a time, the others in halves of it."""
+    dt = DT[dtype]
+    gates = GATES if L < 2000 else GATES[3:5]
+    (Q, K, V, G, beta), S0, dO, dSL = make(1, L, Hk if L < 2000 else 1, len(gates), dk, dv, dt, seed=L)
+    g = torch.Generator().manual_seed(L)
+    G = (torch.tensor(gates, dtype=torch.float64) * (1 + 0.1 * torch.rand(1, L, len(gates), generator=g, dtype=torch.float64))).to(dt).cuda()
+    by_heads(layer, (Q, K, V, G, beta), S0, dO, dSL, dk)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_gate_that_lets_nothing_through_has_no_gradient(layer, dtype):  # noqa: F811
+    """At -256 and below a is 0, and so is its gradient: exactly, among gates of every strength, at a chunk's ends and in its middle, token upon token."""
+    dt = DT[dtype]
+    (Q, K, V, G, beta), S0, dO, dSL = make(2, 200, 2, 4, 64, 64, dt, seed=3)
+    shut = torch.zeros(2, 200, 4, dtype=torch.bool)
+    for t in (0, 1, 15, 16, 31, 47, 48, 63, 64, 100, 127, 128, 199):
+        shut[:, t, t % 4] = shut[1, t, (t + 1) % 4] = True
+    shut[0, 80:90, 2] = True
+    G[shut.cuda()] = torch.tensor([-256.0, -300.0, -1e4, -float("inf")] * 200)[:int(shut.sum())].to(dt).cuda()
+    got = by_heads(layer, (Q, K, V, G, beta), S0, dO, dSL, 64)
+    assert not bool(got[3][shut.cuda()].any()) and bool((got[3][~shut.cuda()] != 0).all())
