@@ -234,7 +234,8 @@ pf_status pf_head_norm_bwd(const void *Q, long long qt, long long qh, const void
  *   O        [N, L, Hv, d_v]                                                 dt     out
  *   SL       [N, Hv, d_v, d_k]                                               fp32   out   NULL: not written.  SL == S0 is allowed
  *   workspace / workspace_bytes   at least pf_gated_delta_workspace_bytes(..., backward = 0, dt) bytes, overwritten; what it holds
- *                                 before does not matter, and nothing in it is kept from call to call
+ *                                 before does not matter, and nothing in it is kept from call to call.  One for N and L does
+ *                                 for calls of fewer sequences and tokens too
  *
  * Packed sequences: Q, K, V, G, beta and O are [L, ...], the rows of all sequences one behind the other (the sequence strides are not looked
  * at), and sequence n is rows offsets[n] .. offsets[n + 1] - 1, any number of them, none too.  Rows that belong to no sequence are

@@ -2,6 +2,7 @@
 #include "../../include/pf_layer.h"
 #include "pf_layer_internal.h"
 
+#include <algorithm>
 #include <limits.h>
 
 namespace {
@@ -264,7 +265,14 @@ extern "C" size_t pf_gated_delta_workspace_bytes(int N, int L, int Hk, int Hv, i
     static const int some = 0;
     a.offsets = packed ? &some : nullptr;
     if (gdelta_sizes(a, dt) != PF_OK || a.chunks == 0) return 0;
-    return pf::gdelta_workspace(a, backward != 0, nullptr);
+    size_t bytes = pf::gdelta_workspace(a, backward != 0, nullptr);
+    // fewer sequences are cut into more segments, or at all, and may take more (none from 29 on: each has 6 chains at least)
+    for (int n = 1; n < N; ++n) {
+        a.N = n;
+        if (gdelta_sizes(a, dt) != PF_OK || a.segments == 1) break;
+        bytes = std::max(bytes, pf::gdelta_workspace(a, backward != 0, nullptr));
+    }
+    return bytes;
 }
 
 extern "C" pf_status pf_gated_delta_fwd(const void *Q, long long qb, long long qt, long long qh, const void *K, long long kb, long long kt,

@@ -407,3 +407,16 @@ def test_offsets_beyond_32_bits(layer):
     pool[slots.long()] = S0
     O = layer.gated_delta_step(*tokens, pool, slots)
     assert torch.equal(O, layer.gated_delta_step(*tokens, S0)) and torch.equal(pool[slots.long()], S0) and not bool(pool[1:2148].any())
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_a_workspace_of_more_sequences(layer, packed):
+    """One that was sized for ten sequences, none of which is cut then, does for two, which are: the same bits as with its own."""
+    heads, dt = (1, 1, 64, 64), torch.bfloat16
+    args, S0, dO, dSL = make(2, 2500, *heads, dt, gate=0.1, rows=(1, 5000) if packed else None)
+    off = torch.tensor([0, 2600, 5000], dtype=torch.int32).cuda() if packed else None
+    want = (*layer.gated_delta_fwd(*args, S0, offsets=off), *layer.gated_delta_bwd(*args, dO, S0, dSL, offsets=off))
+    ws = [torch.empty(layer.pf_gated_delta_workspace_bytes(10, 5000 if packed else 2500, *heads, packed, b, layer.PF_BF16), dtype=torch.uint8, device="cuda") for b in (0, 1)]
+    got = (*layer.gated_delta_fwd(*args, S0, offsets=off, workspace=ws[0]), *layer.gated_delta_bwd(*args, dO, S0, dSL, offsets=off, workspace=ws[1]))
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)

@@ -158,3 +158,18 @@ def test_rotary_table(layer):  # noqa: F811
     angle = torch.arange(7, dtype=torch.float64)[:, None] * 100.0 ** (-torch.tensor([0.0, 2.0, 4.0], dtype=torch.float64) / 6)
     assert t.dtype is torch.float32 and torch.equal(t, torch.cat((angle.cos(), angle.sin()), 1).float())
     assert layer.rotary_table(0, 4, device="cpu").shape == (0, 4) and layer.rotary_table(3, 0, device="cpu").shape == (3, 0)
+
+
+@pytest.mark.parametrize("packed", [0, 1])
+@pytest.mark.parametrize("back", [0, 1])
+def test_a_workspace_does_for_smaller_calls(layer, packed, back):  # noqa: F811
+    """Sized for the most sequences and tokens it is large enough for fewer of either, though what a call takes goes by how its sequences are cut."""
+    for heads in ((1, 1, 128, 128), (1, 1, 64, 32), (1, 2, 256, 256), (2, 6, 72, 40), (1, 1, 1, 1), (5, 5, 200, 16)):
+        for L in (1, 64, 2047, 2048, 4100, 16384, 65536):
+            needs = [layer.pf_gated_delta_workspace_bytes(n, L, *heads, packed, back, BF16) for n in (*range(1, 60), 100, 200)]
+            assert needs == sorted(needs), (heads, L)
+            longer = layer.pf_gated_delta_workspace_bytes(8, L + 1000, *heads, packed, back, BF16)
+            assert longer >= needs[7]
+    for M in (1, 100, 1000, 4096, 8192, 9000, 100000):
+        for Hq, Hk, d in ((32, 8, 128), (17, 1, 72), (1, 0, 16), (70, 9, 256)):
+            assert layer.pf_head_norm_bwd_workspace_bytes(M, Hq, Hk, d, 16) <= layer.pf_head_norm_bwd_workspace_bytes(M + M // 3 + 1, Hq, Hk, d, 16)
