@@ -192,3 +192,30 @@ def test_captured_and_on_another_stream(layer):
         if k == 0:
             for a, b in zip(other, want):
                 assert torch.equal(a, b)
+
+
+def test_every_replay_is_the_eager_call(layer):
+    """A captured call replayed with other inputs, and positions that the table has: the eager call's bits each time, and others than the time before."""
+    how = dict(norm="rms", eps=EPS, q_scale=0.3, pairs=False)
+    Q, K, wq, wk, at, dYq, dYk = make(300, 4, 2, 64, 64, torch.bfloat16, far=900)
+    table = layer.rotary_table(1000, 64)
+
+    def both():
+        return (*layer.head_norm_fwd(Q, K, wq, wk, table, at, **how), *layer.head_norm_bwd(Q, K, dYq, dYk, wq, wk, table, at, **how))
+
+    both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = both()
+    before = None
+    for k in range(4):
+        if k:
+            Q.mul_(0.5).add_(0.1), K.neg_().add_(0.2), at.add_(k), dYq.mul_(1.5), dYk.mul_(-0.5)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, both()):
+            assert bool(torch.isfinite(a).all()) and torch.equal(a, b)
+        if before is not None:
+            assert not any(torch.equal(a, b) for a, b in zip(out, before))
+        before = [t.clone() for t in out]
