@@ -3,7 +3,7 @@
 //
 //   dQ = gamma dO S + (D X) K                      X on and below the diagonal, Y below it
 //   dK = (D X)^T Q + W K + W^T K + delta U R - beta gamma Z S ,   W = beta D Y
-//   dbeta_i = z_i.v_i - gamma_i z_i.S k_i + sum over j of Y_ij D_ij k_i.k_j
+//   dbeta_i = z_i.u_i / beta_i ,  and where beta_i is 0  z_i.v_i - gamma_i z_i.S k_i + sum over j of Y_ij D_ij k_i.k_j
 //   dg_t = sum over i >= t > j of M_ij + sum over i >= t of (gamma_i do_i.S q_i - beta_i gamma_i z_i.S k_i)
 //          + sum over j < t of delta_j u_j.R k_j + gamma_64 <R, S> ,   M = X P + Y A .
 //
@@ -43,7 +43,7 @@ __global__ __launch_bounds__(512) void grad_kernel(GDelta a)
     __shared__ __attribute__((aligned(16))) char states[2][StateTile::kBytes], values[UTile::kBytes], tokens[2][kTokens], pairs[2][PairTile::kBytes];
     __shared__ __attribute__((aligned(16))) float rows[3][C];      // gamma, delta, beta
     __shared__ float coarse[C], fine[C];
-    __shared__ float srow[2][C], sstate[2][C], slater[2][C], sbeta[2][C], scol[4][C], sdot[8];
+    __shared__ float srow[2][C], sstate[2][C], slater[2][C], sbeta[2][C], szu[C], scol[4][C], sdot[8];
     const StateTile Ss = {reinterpret_cast<T *>(states[0])}, Rs = {reinterpret_cast<T *>(states[1])};
     const UTile Us = {reinterpret_cast<T *>(values)};
     T *Ks = reinterpret_cast<T *>(tokens[0]), *Qs = reinterpret_cast<T *>(tokens[1]);
@@ -208,6 +208,7 @@ __global__ __launch_bounds__(512) void grad_kernel(GDelta a)
                         w1[e] = in && j <= i ? D * X[m][e] : 0.f;
                         const float y = in && j < i ? -Y[m][e] * D : 0.f;
                         w2[e] = beta[e] * y;
+                        if (j == i) szu[i] = Y[m][e];
                         yk[e] += y * kk[m][e];
                         below[e] = sum += (in && j < i ? X[m][e] * p[e] : 0.f) + w2[e] * kk[m][e];
                     }
@@ -323,7 +324,10 @@ __global__ __launch_bounds__(512) void grad_kernel(GDelta a)
         if (lane < x.len) {
             const long long to = out_row(a, x.seq, x.tok + lane) * a.Hv + h;
             static_cast<T *>(a.dG)[to] = (T)e;
-            static_cast<T *>(a.dbeta)[to] = (T)(sbeta[0][lane] + sbeta[1][lane]);
+            // u = beta (v - what the state has for k): that difference has been taken, in 24 bits; the other form takes it of sums whose operands have 16.
+            // (Below 2^-60 numbers may end before u does.)
+            const float beta = rows[2][lane];
+            static_cast<T *>(a.dbeta)[to] = (T)(fabsf(beta) > 0x1p-60f ? szu[lane] / beta : sbeta[0][lane] + sbeta[1][lane]);
         }
     }
 }

@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import gated_delta_ref as ref
-from test_gpu_gated_delta import DT, bound, layer, make, wide  # noqa: F401  (layer: fixture)
+from test_gpu_gated_delta import DT, bound, f32_bound, layer, make, wide  # noqa: F401  (layer: fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -49,3 +49,31 @@ def test_a_gate_that_lets_nothing_through_has_no_gradient(layer, dtype):  # noqa
     G[shut.cuda()] = torch.tensor([-256.0, -300.0, -1e4, -float("inf")] * 200)[:int(shut.sum())].to(dt).cuda()
     got = by_heads(layer, (Q, K, V, G, beta), S0, dO, dSL, 64)
     assert not bool(got[3][shut.cuda()].any()) and bool((got[3][~shut.cuda()] != 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("L,dk,dv", [(60, 64, 64), (100, 128, 32), (200, 256, 40), (40, 72, 16)])
+def test_gradient_of_beta_where_the_state_knows_the_values(layer, L, dk, dv, dtype):  # noqa: F811
+    """e_t = v_t - S k_t is 2^-12 of either, and dbeta_t = e_t.R k_t as small.  Keys are unit vectors, each token its own, g = 0 and beta a power of two or 0, so that
+    e_t comes out exact in fp32, and what is left are the roundings that the tolerances count."""
+    g, dt = torch.Generator().manual_seed(L), DT[dtype]
+    n = lambda *s: torch.randn(s, generator=g, dtype=torch.float64)  # noqa: E731
+    i = lambda lo, hi, *s: torch.randint(lo, hi, s, generator=g).double()  # noqa: E731
+    Q, K = torch.nn.functional.normalize(n(1, L, 1, dk), dim=-1), torch.eye(dk, dtype=torch.float64)[torch.randperm(dk, generator=g)[:L]][None, :, None]
+    V = i(-120, 121, 1, L, 1, dv) / 64
+    e = (i(0, 2, L, dv) * 2 - 1) * (1 + i(0, 64, L, dv) / 64) * 2.0 ** -12
+    beta = 2.0 ** -i(0, 3, 1, L, 1)
+    beta[0, ::7] = 0
+    S0 = 0.3 * n(1, 1, dv, dk)
+    S0[0, 0] = torch.where(K[0, :, 0].sum(0) > 0, (V[0, :, 0] - e).t() @ K[0, :, 0], S0[0, 0])
+    dO, dSL = n(1, L, 1, dv), n(1, 1, dv, dk)
+    args = [t.to(dt).cuda() for t in (Q, K, V, torch.zeros(1, L, 1), beta)]
+    dO, S0, dSL = dO.to(dt).cuda(), S0.float().cuda(), dSL.float().cuda()
+    got = layer.gated_delta_bwd(*args, dO, S0, dSL)[4]
+    want = ref.delta_grads(wide(*args, S0), *wide(dO, dSL))[4]
+    some = beta[0, :, 0] > 0
+    assert ref.off(got[0, some], want[0, some]) <= bound(dt, dk)
+    # where beta is 0 the difference is taken of sums over d_v and pairs of tokens: its terms are |z| |v| at most, z = R k
+    R = float(dSL.double().norm()) + float(dO.double().norm(dim=-1).sum())
+    tol = (4 * 2.0 ** -17 if dtype == "bf16" else f32_bound(dk)) * R * float(V.norm(dim=-1).max()) + bound(dt, dk) * float(want[0, ~some].norm())
+    assert float((got[0, ~some].double().cpu() - want[0, ~some]).norm()) <= tol
