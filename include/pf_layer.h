@@ -265,6 +265,9 @@ pf_status pf_gated_delta_fwd(const void *Q, long long qb, long long qt, long lon
  *
  * with dq and dk summed over the heads that share them.  (A g beyond -256 or 256 has the gradient of the bound that it counts as.)
  *
+ * The states, R, dV and dS0 are computed in fp32 (24 bits).  What goes into dQ, dK, dG and dbeta alone has, for dt = PF_BF16, 16 bits at least (S, R,
+ * what the tokens write, Z, and the products of pairs of tokens), summed in fp32.
+ *
  *   dO        [N, L, Hv, d_v], strides ob, ot, oh          dt     in
  *   dSL       [N, Hv, d_v, d_k]                            fp32   in    NULL: zeros
  *   dQ, dK    [N, L, Hk, d_k]                              dt     out
