@@ -245,8 +245,12 @@ pf_status pf_head_norm_bwd(const void *Q, long long qt, long long qh, const void
  * Heads: Hk divides Hv; d_k and d_v up to 256 (pf_gated_delta_supported; else PF_ERR_UNSUPPORTED, Hv not a multiple of Hk: PF_ERR_SHAPE).
  * States and all that goes into them are computed in fp32 (24 bits); what goes into O alone with 16 bits at least for dt = PF_BF16.  L up to
  * 2^30.  No tokens: SL receives S0 (or zeros), and the sequence pointers may be NULL.  N == 0: nothing is done.
- * Few long sequences are cut into segments that run side by side, joined by what each makes of the unit matrix: where gates above 0 take that
- * beyond fp32 (sums of g beyond 88 that nothing erases), a state of zeros becomes NaN as well.  Cut or not goes by the sizes alone.
+ * g is meant to be 0 at most.  Above 0 it is used as given, but with s the largest sum of gates of neighbouring tokens within a chunk the chunk's
+ * products have factors e^s also where beta erases what the gates let grow: errors are up to e^s times those without, and from s = 88 on results may be
+ * NaN where the formula's are finite, those of a state of zeros among them.  pf_gated_delta_step multiplies token by token and has none of this.
+ * Few long sequences are cut into segments that run side by side, joined by what each makes of the unit matrix: where gates above 0, or keys with
+ * beta |k|^2 above 2, take that beyond fp32 (sums of g beyond 88 that nothing erases), a state of zeros becomes NaN as well.  Cut or not goes by the
+ * sizes alone.
  * NaN and infinities in a token reach all later ones, and may reach the outputs of those up to 63 before it whose chunk it shares.
  */
 int pf_gated_delta_supported(int Hk, int Hv, int d_k, int d_v, pf_dtype dt);

@@ -584,6 +584,7 @@ def gated_delta_fwd(Q, K, V, G, beta, S0=None, *, offsets=None, workspace=None):
     Q, K [B, L, Hk, dk], V [B, L, Hv, dv], G, beta [B, L, Hv] (float32 or bfloat16, in any order of the outer dimensions), S0 [B, Hv, dv,
     dk] float32 or None.  Hv / Hk heads of values share a head of queries and keys.  With offsets [N + 1] (int32, on the device) B is 1 and
     sequence n is rows offsets[n] .. offsets[n + 1] - 1, S0 [N, Hv, dv, dk]; O's rows of no sequence are not written.
+    G is meant to be 0 at most: sums above 0 within 64 tokens, s at most, make errors e^s times larger, and NaN from 88 on.
     Returns (O [B, L, Hv, dv], S_L like S0)."""
     dt, index, sizes, arrays, sp, op = _gated_delta_of(Q, K, V, G, beta, S0, offsets)
     N, L, Hk, Hv, dk, dv = sizes

@@ -77,3 +77,33 @@ def test_gradient_of_beta_where_the_state_knows_the_values(layer, L, dk, dv, dty
     R = float(dSL.double().norm()) + float(dO.double().norm(dim=-1).sum())
     tol = (4 * 2.0 ** -17 if dtype == "bf16" else f32_bound(dk)) * R * float(V.norm(dim=-1).max()) + bound(dt, dk) * float(want[0, ~some].norm())
     assert float((got[0, ~some].double().cpu() - want[0, ~some]).norm()) <= tol
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("s", [0.5, 3.0])
+def test_gates_above_zero(layer, s, dtype):  # noqa: F811
+    """Sums of gates of a chunk up to s: the tolerances times e^s, as a chunk's products have e^s for a factor also where beta erases what the gates let grow."""
+    dt = DT[dtype]
+    (Q, K, V, _, beta), S0, dO, dSL = make(1, 130, 1, 2, 64, 32, dt, seed=5)
+    beta[:, :, 1] = 1.0
+    g = torch.Generator().manual_seed(5)
+    G = (torch.rand(1, 130, 2, generator=g) * (s / 64)).to(dt).cuda()
+    O, SL = layer.gated_delta_fwd(Q, K, V, G, beta, S0)
+    grads = layer.gated_delta_bwd(Q, K, V, G, beta, dO, S0, dSL)
+    wide_args = wide(Q, K, V, G, beta, S0)
+    want = (*ref.delta(*wide_args), *ref.delta_grads(wide_args, *wide(dO, dSL)))
+    for i, (a, b) in enumerate(zip((O, SL, *grads), want)):
+        assert ref.off(a, b) <= bound(a.dtype, 64) * 2.718281828 ** s, i
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_token_by_token_gates_may_be_large(layer, dtype):  # noqa: F811
+    """k = 1, beta = 1: every token erases what its gate of e^2 let grow, S_t = v_t, over any number of tokens."""
+    dt = DT[dtype]
+    V = torch.randn(2, 200, 1, 5, generator=torch.Generator().manual_seed(1)).to(dt).cuda()
+    one, two, S = (torch.full(s, v, dtype=t, device="cuda") for s, v, t in (((2, 1, 1), 1.0, dt), ((2, 1), 2.0, dt), ((2, 1, 5, 1), 0.0, torch.float32)))
+    for t in range(200):
+        o = layer.gated_delta_step(one, one, V[:, t], two, one[..., 0], S)
+        # v - a S + a S: three roundings of a S, at most e^2 times the token's before
+        tol = 4 * 2.0 ** -24 * 7.39 * float(V.abs().max()) * 2
+        assert float((S[..., 0] - V[:, t].float()).abs().max()) <= tol and float((o.float() - V[:, t].float()).abs().max()) <= tol + 2.0 ** -8 * float(V.abs().max())
