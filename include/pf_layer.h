@@ -203,6 +203,9 @@ pf_status pf_head_norm_fwd(const void *Q, long long qt, long long qh, const void
  *
  *   dx = (g - xh m) / n ,  m = mean(g xh) (PF_NORM_RMS) or sum(g xh) (PF_NORM_L2) ,     dw = sum over tokens and heads of t xh
  *
+ * A position that the table does not have gives NaN in its token's rows of dx, and so in dw of the values that turn: such tokens' rows are left out of the call
+ * where dw is wanted.
+ *
  *   dYq, dYk   [M, Hq, d], [M, Hk, d], strides ..t, ..h    dt     in
  *   dQ, dK     [M, Hq, d], [M, Hk, d]                      dt     out   dQ == dYq or dQ == Q (dK ..) is allowed where that is dense
  *   dwq, dwk   [d]                                         fp32   out   NULL: not wanted (neither: no workspace).  No rows: zeros

@@ -219,3 +219,18 @@ def test_every_replay_is_the_eager_call(layer):
         if before is not None:
             assert not any(torch.equal(a, b) for a, b in zip(out, before))
         before = [t.clone() for t in out]
+
+
+def test_gradients_at_a_position_that_the_table_does_not_have(layer):
+    """NaN in the token's own rows and in what dw sums over them, of the turned values; every other number is as without the token."""
+    how = dict(norm="rms", eps=EPS, q_scale=0.5, pairs=False)
+    Q, K, wq, wk, at, dYq, dYk = make(9, 2, 1, 64, 32, torch.float32)
+    table = layer.rotary_table(1000, 32)
+    at[4] = -1
+    dQ, dK, dwq, dwk = layer.head_norm_bwd(Q, K, dYq, dYk, wq, wk, table, at, **how)
+    there = [0, 1, 2, 3, 5, 6, 7, 8]
+    want = layer.head_norm_bwd(*(t[there] for t in (Q, K, dYq, dYk)), wq, wk, table, at[there], **how)
+    for got, w in ((dQ, want[0]), (dK, want[1])):
+        assert bool(got[4].isnan().all()) and torch.equal(got[there], w)
+    for got in (dwq, dwk):
+        assert bool(got[:32].isnan().all()) and bool(torch.isfinite(got[32:]).all())
