@@ -679,7 +679,9 @@ template <typename T, int DK, bool FULL> void scan(const GDelta &a, int what, bo
         scan_kernel<T, DK, FULL, kEnds><<<grid, 512, 0, stream>>>(a);
     } else {
         // Backward: a third group of wavefronts where every workgroup has a compute unit for itself (2 x 8192 tokens, 16 heads of 128: 383 ->
-        // 373 us; of three groups no two workgroups have their registers there).  Wider or fp32: their values do not fit a third group's.
+        // 373 us; d_k up to 64: of three groups no two workgroups have their registers there.  Of 128 none have their LDS anyway, 103 KB, and with more
+        // workgroups than compute units three groups are faster as well: the whole backward of 4 x 4096 tokens of 16 heads 1148 -> 1062 us.  That is not taken yet).
+        // Wider or fp32: their values do not fit a third group's.
         if constexpr (sizeof(T) == 2 && DK <= 128)
             if (grid.x <= (unsigned)device_cu_count()) {
                 scan_bwd_kernel<T, DK, FULL, 3><<<grid, 768, 0, stream>>>(a, ends);

@@ -100,7 +100,9 @@ inline bool gdelta_full(const GDelta &a, int size)
 // columns, and what joins them takes them one after the other.  Of that first run two workgroups to a compute unit at most, eight chunks to a
 // segment at least, and no more segments than make a step of the join (1.7 us) worth the chunks (1.5 us, twice) that it saves; it pays from three
 // segments and 32 chunks on.  bf16, heads of 128, forward, cut and whole: 65536 tokens of one head 215 and 1554 us, of four 586 and 1893, of eight
-// 1122 and 2009; 2048 tokens of one head 49 and 63, 1600 in three segments 51 and 51 (their backward 138 and 121).
+// 1122 and 2009; 2048 tokens of one head 49 and 63, 1600 in three segments 51 and 51 (their backward 138 and 121).  Backward: 16384 tokens of one head
+// 250 and 881, of eight 866 and 1155, 2048 of one 125 and 147.  fp32: 65536 of one 366 and 3474, 2048 78 and 127, backward 196 and 263.  Heads of 64: 65536 of four
+// 265 and 1367, 2048 of one 43 and 52, backward 98 and 122; of 256: 65536 of one 557 and 2587, 2048 91 and 98, backward 252 and 251 (nothing there).
 inline int gdelta_segments(const GDelta &a)
 {
     if (a.chunks == 0 || a.N == 0) return 1;
