@@ -487,6 +487,8 @@ def _free(t, what, shape, dtype, index):
 def rotary_table(length: int, rot: int, *, base: float = 10000.0, device="cuda"):
     """Cosines and sines of positions 0 .. length - 1 for head_norm_fwd, [length, rot] in float32: pair i turns by base^(-2 i / rot)
     for each position (angles in float64, since those of far positions need more than 24 bits)."""
+    if length < 0 or rot < 0 or rot % 2:
+        raise ValueError("length and rot must not be negative, and rot even")
     turn = torch.arange(length, dtype=torch.float64)[:, None] * base ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)
     return torch.cat((turn.cos(), turn.sin()), 1).float().to(device)
 

@@ -173,3 +173,10 @@ def test_a_workspace_does_for_smaller_calls(layer, packed, back):  # noqa: F811
     for M in (1, 100, 1000, 4096, 8192, 9000, 100000):
         for Hq, Hk, d in ((32, 8, 128), (17, 1, 72), (1, 0, 16), (70, 9, 256)):
             assert layer.pf_head_norm_bwd_workspace_bytes(M, Hq, Hk, d, 16) <= layer.pf_head_norm_bwd_workspace_bytes(M + M // 3 + 1, Hq, Hk, d, 16)
+
+
+@pytest.mark.parametrize("length,rot", [(5, 3), (5, -2), (-1, 4), (5, 1)])
+def test_rotary_table_refuses(layer, length, rot):  # noqa: F811
+    """An odd number of columns would come out as one more, with another pair's angles."""
+    with pytest.raises(ValueError, match="even"):
+        layer.rotary_table(length, rot, device="cpu")
