@@ -29,7 +29,7 @@ template <typename T> __device__ __forceinline__ In<T> kept(In<T> x, bool keep)
 // A workgroup of eight wavefronts for each chunk and value head; wavefronts w and w + 4 have the tokens 16 w .., of each result one half of the
 // columns.  COLS columns (of d_k) of the gradients at a time, so all of them up to 128: with 32 rows (of d_v) of S, R and U in LDS the products with
 // them, the first time X and Y too, so that each is read once; then W1 = D X and W, which stay in LDS, and the products with K and Q.
-// What bounds it is memory, 310 KB a workgroup at 128 x 128 in bf16: 4096 of them take 410 us, 3.1 TB/s (with 64 columns at a time, U and Z
+// What bounds it is memory, 310 KB a workgroup at 128 x 128 in bf16: 4096 of them take 392 us, 3.3 TB/s (with 64 columns at a time, U and Z
 // read three times, 575; of four wavefronts and no load ahead 640).  One workgroup to a compute unit, by its registers and by its LDS
 // (119 KB of 160 in bf16, 87 with 64 columns), though not all of that is in use at any one time.
 // Where heads share Q and K, their parts of dQ and dK take the place of S and R in the workspace, and share_kernel adds them.
