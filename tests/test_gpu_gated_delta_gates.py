@@ -28,10 +28,10 @@ def by_heads(layer, args, S0, dO, dSL, dk):  # noqa: F811
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("L,Hk,dk,dv", [(64, 8, 64, 64), (130, 4, 128, 32), (70, 8, 72, 40), (150, 2, 256, 64), (2100, 1, 64, 32)])
 def test_each_head_a_gate_of_its_own(layer, L, Hk, dk, dv, dtype):  # noqa: F811
-    """The last size in segments: two of the gates at a time, the others in halves of it."""
+    """Around each of GATES; the last size is cut into segments and has two of them."""
     dt = DT[dtype]
     gates = GATES if L < 2000 else GATES[3:5]
-    (Q, K, V, G, beta), S0, dO, dSL = make(1, L, Hk if L < 2000 else 1, len(gates), dk, dv, dt, seed=L)
+    (Q, K, V, G, beta), S0, dO, dSL = make(1, L, Hk, len(gates), dk, dv, dt, seed=L)
     g = torch.Generator().manual_seed(L)
     G = (torch.tensor(gates, dtype=torch.float64) * (1 + 0.1 * torch.rand(1, L, len(gates), generator=g, dtype=torch.float64))).to(dt).cuda()
     by_heads(layer, (Q, K, V, G, beta), S0, dO, dSL, dk)
